@@ -625,6 +625,117 @@ PA_API pa_status pa_gmm_eps_noalloc(const float* means_dev, int K, int64_t D, do
                                     const float* batch_x_dev, const int32_t* miss_bt_dev,
                                     int n_rows, float* batch_eps_dev, void* stream);
 
+/* ---- layers of a text-conditioned denoiser ---------------------------------
+ * The conditioning part of a denoiser for the solver's batch, forward and
+ * backward (gradients serve guidance through the denoiser and the fitting of
+ * the conditioning or of the weights): the norm in front of a cross attention
+ * and the attention to a text encoder's states. A miss batch holds many
+ * timesteps of few trajectories, so keys and values are given per trajectory
+ * and picked by the miss list's first column, and the number of rows that count
+ * may stay on the device (pa_n_miss_dev), as in a captured loop. The paper has
+ * no counterpart; its Sec. 3.2 denoisers contain these layers.
+ *
+ * Calls are asynchronous on `stream`, allocate nothing, keep nothing and may be
+ * captured (after one call outside a capture on the device, which loads the
+ * kernels). Every tensor is a DEVICE pointer on the current device; its last
+ * axis is contiguous and the other strides are given in elements. Arithmetic is
+ * fp32, results are rounded once to the tensor's type; of the values in between,
+ * the attention's probabilities and their gradients enter the second products
+ * in the tensors' 16-bit type. Results do not depend on timing: the same call
+ * gives the same bits. Workspaces must be 256-byte aligned and may be reused by
+ * the next call on the same stream.
+ * ------------------------------------------------------------------------ */
+#define PA_F32 0
+#define PA_F16 1
+#define PA_BF16 2
+
+/* Layer norm over the last axis of x [rows][cols] (row stride x_stride):
+ *   mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps), y = (x - mu) r weight + bias.
+ * dtype: PA_F32, PA_F16 or PA_BF16 of x, weight, bias and y. weight, bias:
+ * [cols], NULL: ones, zeros. mean, rstd: fp32 [rows], written for the backward
+ * pass; both or neither may be NULL. y may be x itself (same stride), or
+ * must not overlap it. n_items_dev (DEVICE int32, NULL: all rows): only the
+ * first *n_items_dev * rows_per_item rows are read and written; rows must be a
+ * multiple of rows_per_item (>= 1, ignored without n_items_dev). Any cols >= 1;
+ * rows whose addresses are multiples of 16 bytes are fastest. */
+PA_API pa_status pa_layer_norm(int dtype, int64_t rows, int cols, const void* x, int64_t x_stride,
+                               const void* weight, const void* bias, double eps, void* y, int64_t y_stride,
+                               float* mean, float* rstd, const int32_t* n_items_dev, int64_t rows_per_item,
+                               void* stream);
+
+/* Bytes of device workspace that pa_layer_norm_backward needs for dweight and
+ * dbias (0 on bad sizes). */
+PA_API size_t pa_layer_norm_backward_workspace_bytes(int64_t rows, int cols);
+
+/* Gradients of pa_layer_norm for dy [rows][cols], from x, mean and rstd of the
+ * forward call: with xh = (x - mu) r and g = dy weight,
+ *   dx = r (g - mean g - xh mean(g xh)),  dweight = sum dy xh,  dbias = sum dy
+ * (sums over the rows that count). dweight and dbias [cols] of type dtype may
+ * each be NULL; with both NULL no workspace is needed. dx may be dy or x itself
+ * (same stride), or must not overlap them. */
+PA_API pa_status pa_layer_norm_backward(int dtype, int64_t rows, int cols, const void* dy, int64_t dy_stride,
+                                        const void* x, int64_t x_stride, const void* weight, const float* mean,
+                                        const float* rstd, void* dx, int64_t dx_stride, void* dweight, void* dbias,
+                                        const int32_t* n_items_dev, int64_t rows_per_item, void* workspace_dev,
+                                        size_t workspace_bytes, void* stream);
+
+/* Cross attention of items (rows of the miss batch) to their sources' states.
+ * Query row (n, t, h) of q [items][tokens][heads][head_dim] attends to the keys
+ * of source g = source[n * source_stride] (NULL: g = n, sources >= items), key
+ * head j = h / (heads / kv_heads) of k, v [sources][keys][kv_heads][head_dim]:
+ *   s_i = scale q . k_i,  p_i = exp(s_i - max s),  out = sum p_i v_i / sum p_i,
+ *   lse = max s + ln sum p_i,
+ * over the keys i < lengths[g] (NULL: all; values are clamped to [0, keys]) with
+ * mask[g * mask_stride + i] != 0 (NULL: all). Keys that do not count are not
+ * read. A row without keys gives out = 0 and lse = -inf, and no gradient.
+ * Strides (item, token, head) are in elements and multiples of 8, the tensors
+ * 16-byte aligned; head_dim a multiple of 8, 8 to 256; kv_heads divides heads.
+ * Only items n < *n_items_dev (NULL: all) are computed. */
+typedef struct {
+  int32_t dtype;               /* PA_F16 or PA_BF16 */
+  int32_t items, tokens;       /* of the queries */
+  int32_t sources, keys;
+  int32_t heads, kv_heads, head_dim;
+  double scale;                /* finite, > 0 */
+  const void *q, *k, *v;
+  int64_t q_stride[3], k_stride[3], v_stride[3];   /* item (k, v: source), token, head */
+  const int32_t* source;       /* DEVICE; an index outside [0, sources) leaves its item without keys */
+  int64_t source_stride;       /* and is reported by pa_attention_check */
+  const int32_t* lengths;      /* DEVICE [sources] */
+  const uint8_t* mask;         /* DEVICE [sources][mask_stride] */
+  int64_t mask_stride;
+  const int32_t* n_items_dev;  /* DEVICE */
+  void* out;                   /* forward: written; backward: read */
+  int64_t out_stride[3];
+  float* lse;                  /* [items][tokens][heads]; forward: written, may be NULL; backward: read */
+  /* backward only */
+  const void* dout;            /* as out */
+  void *dq, *dk, *dv;          /* as q, k, v; all three are written, dk and dv for every source and key */
+  int64_t dout_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
+} pa_attention_t;
+
+/* Bytes of device workspace of pa_attention (backward = 0) or
+ * pa_attention_backward (1) for these sizes; only the sizes, head_dim and
+ * whether mask is NULL matter. (size_t)-1 on bad sizes; 0: none needed. */
+PA_API size_t pa_attention_workspace_bytes(const pa_attention_t* a, int backward);
+
+PA_API pa_status pa_attention(const pa_attention_t* a, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* Gradients, from out and lse of the forward call on the same inputs:
+ *   p_i = exp(s_i - lse), ds_i = p_i (dout . v_i - dout . out),
+ *   dq = scale sum_i ds_i k_i,  dk_i = scale sum ds_i q,  dv_i = sum p_i dout,
+ * the last two over all rows of all items of the source that count and all
+ * heads that share the key head. In PA_F16 a value of ds below 2^-24 is lost, as
+ * is usual: scale the loss. */
+PA_API pa_status pa_attention_backward(const pa_attention_t* a, void* workspace_dev, size_t workspace_bytes,
+                                       void* stream);
+
+/* Synchronise `stream`, report the first device-side failure of the attention
+ * calls on this device since the last check, and clear it: PA_ERR_DEVICE for a
+ * source index out of range, PA_ERR_TIMEOUT for a bounded wait that ran out
+ * (the outputs of that call are not valid). */
+PA_API pa_status pa_attention_check(void* stream);
+
 /* ---- misc -------------------------------------------------------------- */
 
 PA_API const char* pa_status_string(int status);

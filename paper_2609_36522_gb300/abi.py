@@ -48,6 +48,21 @@ class PaSrdsStats(C.Structure):
         return {k: getattr(self, k) for k, _ in self._fields_ if k != "reserved"}
 
 
+class PaAttention(C.Structure):
+    """pa_attention_t; the fields behind ``lse`` are the backward pass's."""
+    _fields_ = [("dtype", C.c_int32), ("items", C.c_int32), ("tokens", C.c_int32), ("sources", C.c_int32),
+                ("keys", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("scale", C.c_double), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("source", C.c_void_p), ("source_stride", C.c_int64), ("lengths", C.c_void_p), ("mask", C.c_void_p),
+                ("mask_stride", C.c_int64), ("n_items_dev", C.c_void_p), ("out", C.c_void_p),
+                ("out_stride", C.c_int64 * 3), ("lse", C.c_void_p), ("dout", C.c_void_p), ("dq", C.c_void_p),
+                ("dk", C.c_void_p), ("dv", C.c_void_p), ("dout_stride", C.c_int64 * 3), ("dq_stride", C.c_int64 * 3),
+                ("dk_stride", C.c_int64 * 3), ("dv_stride", C.c_int64 * 3)]
+
+
+PA_F32, PA_F16, PA_BF16 = 0, 1, 2
+
 _lib = None
 VP = C.c_void_p
 PVP = C.POINTER(C.c_void_p)
@@ -113,6 +128,15 @@ _PROTOS = {
     "pa_gmm_destroy": (None, [VP]),
     "pa_gmm_eps_noalloc": (C.c_int, [VP, C.c_int, C.c_int64, C.c_double, C.POINTER(C.c_double),
                                      C.c_int, VP, VP, C.c_int, VP, VP]),
+    "pa_layer_norm": (C.c_int, [C.c_int, C.c_int64, C.c_int, VP, C.c_int64, VP, VP, C.c_double, VP, C.c_int64, VP, VP,
+                                VP, C.c_int64, VP]),
+    "pa_layer_norm_backward_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int]),
+    "pa_layer_norm_backward": (C.c_int, [C.c_int, C.c_int64, C.c_int, VP, C.c_int64, VP, C.c_int64, VP, VP, VP, VP,
+                                         C.c_int64, VP, VP, VP, C.c_int64, VP, C.c_size_t, VP]),
+    "pa_attention_workspace_bytes": (C.c_size_t, [C.POINTER(PaAttention), C.c_int]),
+    "pa_attention": (C.c_int, [C.POINTER(PaAttention), VP, C.c_size_t, VP]),
+    "pa_attention_backward": (C.c_int, [C.POINTER(PaAttention), VP, C.c_size_t, VP]),
+    "pa_attention_check": (C.c_int, [VP]),
     "pa_status_string": (C.c_char_p, [C.c_int]),
     "pa_last_error": (C.c_char_p, []),
 }
@@ -460,3 +484,43 @@ def pa_srds_errors(h, n_blocks, batch):
 
 def pa_srds_destroy(h):
     lib().pa_srds_destroy(h)
+
+
+# ---- layers of a text-conditioned denoiser ----------------------------------
+
+def pa_layer_norm(dtype, rows, cols, x_ptr, x_stride, weight_ptr, bias_ptr, eps, y_ptr, y_stride, mean_ptr, rstd_ptr,
+                  n_items_dev_ptr, rows_per_item, stream_ptr):
+    return _check("pa_layer_norm", lib().pa_layer_norm(
+        dtype, rows, cols, x_ptr, x_stride, weight_ptr, bias_ptr, eps, y_ptr, y_stride, mean_ptr, rstd_ptr,
+        n_items_dev_ptr, rows_per_item, stream_ptr))
+
+
+def pa_layer_norm_backward_workspace_bytes(rows, cols):
+    return int(lib().pa_layer_norm_backward_workspace_bytes(rows, cols))
+
+
+def pa_layer_norm_backward(dtype, rows, cols, dy_ptr, dy_stride, x_ptr, x_stride, weight_ptr, mean_ptr, rstd_ptr, dx_ptr,
+                           dx_stride, dweight_ptr, dbias_ptr, n_items_dev_ptr, rows_per_item, workspace_ptr,
+                           workspace_bytes, stream_ptr):
+    return _check("pa_layer_norm_backward", lib().pa_layer_norm_backward(
+        dtype, rows, cols, dy_ptr, dy_stride, x_ptr, x_stride, weight_ptr, mean_ptr, rstd_ptr, dx_ptr, dx_stride,
+        dweight_ptr, dbias_ptr, n_items_dev_ptr, rows_per_item, workspace_ptr, workspace_bytes, stream_ptr))
+
+
+def pa_attention_workspace_bytes(a, backward):
+    n = int(lib().pa_attention_workspace_bytes(a, int(backward)))
+    if n == C.c_size_t(-1).value:
+        raise PaError("pa_attention_workspace_bytes", PA_ERR_ARG, last_error())
+    return n
+
+
+def pa_attention(a, workspace_ptr, workspace_bytes, stream_ptr):
+    return _check("pa_attention", lib().pa_attention(a, workspace_ptr, workspace_bytes, stream_ptr))
+
+
+def pa_attention_backward(a, workspace_ptr, workspace_bytes, stream_ptr):
+    return _check("pa_attention_backward", lib().pa_attention_backward(a, workspace_ptr, workspace_bytes, stream_ptr))
+
+
+def pa_attention_check(stream_ptr):
+    return _check("pa_attention_check", lib().pa_attention_check(_dptr(stream_ptr)))

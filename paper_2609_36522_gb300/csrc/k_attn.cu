@@ -1,0 +1,322 @@
+// Cross attention, forward: rows of queries (item n, token t, head h) attend to
+// the states of the item's source,
+//   s_j = scale q . k_j,  p_j = exp(s_j - max s),  o = sum p_j v_j / sum p_j,
+// over the source's keys that count; lse = max s + ln sum p_j.
+#include "pa_attn.cuh"
+
+namespace pa {
+namespace {
+
+__device__ int32_t g_status;
+
+// ---------------------------------------------------------------------------
+// The keys of each source that count, in order; a CTA per source.
+constexpr int kListThreads = 256;
+__global__ void __launch_bounds__(kListThreads) k_attn_keys(const uint8_t* __restrict__ mask, int64_t stride,
+                                                           const int32_t* __restrict__ len, int K, int32_t* __restrict__ n,
+                                                           int32_t* __restrict__ list) {
+  __shared__ int s_n[kListThreads / 32];
+  pdl_wait();
+  pdl_trigger();
+  const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int end = len ? min(max(len[g], 0), K) : K;
+  const uint8_t* m = mask + g * stride;
+  int base = 0;
+  for (int k0 = 0; k0 < end; k0 += kListThreads) {
+    const int k = k0 + threadIdx.x;
+    const bool in = k < end && m[k] != 0;
+    const unsigned b = __ballot_sync(0xffffffffu, in);
+    if (lane == 0) s_n[warp] = __popc(b);
+    __syncthreads();
+    int before = base;
+#pragma unroll
+    for (int w = 0; w < kListThreads / 32; ++w) {
+      const int c = s_n[w];
+      if (w < warp) before += c;
+      base += c;
+    }
+    if (in) list[(int64_t)g * K + before + __popc(b & ((1u << lane) - 1))] = k;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) n[g] = base;
+}
+
+// ---------------------------------------------------------------------------
+// CUDA cores: RT rows of one key head per CTA. The lanes of a group of `gs`
+// hold eight values each of a key; a warp works on 32 / gs keys at a time, four
+// times that at once, every group with a running maximum and sum of its own;
+// groups and warps are joined at the end.
+constexpr int kRowWarps = 8;
+constexpr int kRowKeys = 4;  // keys in flight per group
+
+template <typename T, int RT>
+__global__ void __launch_bounds__(kRowWarps * 32) k_attn_rows(AttnArgs a, Keys keys, int gs, int chunks, int splits,
+                                                             float* __restrict__ po, float* __restrict__ pl) {
+  extern __shared__ float smem[];  // [warp][RT][D], then [warp][RT] maxima and sums
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int at = lane & (gs - 1), kpw = 32 / gs, R = a.H / a.J;
+  pdl_wait();
+  pdl_trigger();
+  int64_t b = blockIdx.x;
+  const int chunk = (int)(b % chunks);
+  b /= chunks;
+  const int j = (int)(b % a.J), n = (int)(b / a.J);
+  if (n >= items_of(a.count, a.N)) return;
+  const int g = source_of(a.src, a.src_stride, n, a.G, a.status);
+  const int kn = g < 0 ? 0 : keys.count(g);
+  const int lo = (int)((int64_t)kn * blockIdx.y / splits), hi = (int)((int64_t)kn * (blockIdx.y + 1) / splits);
+  const float c2 = a.scale * kLog2e;
+  float q[RT][8], acc[RT][8], m[RT], l[RT];
+  const bool col = at * 8 < a.D;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int64_t row = (int64_t)chunk * RT + r;
+    const int t = (int)(row / R), h = j * R + (int)(row % R);
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (t < a.Q && col)
+      u = *reinterpret_cast<const uint4*>((const T*)a.q + n * a.qs.item + t * a.qs.token + h * a.qs.head + at * 8);
+    Elem<T>::open(u, q[r]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      q[r][i] *= c2;
+      acc[r][i] = 0.f;
+    }
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+  }
+  const T* kp = (const T*)a.k + (int64_t)max(g, 0) * a.ks.item + j * a.ks.head + at * 8;
+  const T* vp = (const T*)a.v + (int64_t)max(g, 0) * a.vs.item + j * a.vs.head + at * 8;
+  for (int k0 = lo + warp * kpw * kRowKeys; k0 < hi; k0 += kRowWarps * kpw * kRowKeys) {
+    uint4 ku[kRowKeys], vu[kRowKeys];
+    bool in[kRowKeys];
+#pragma unroll
+    for (int u = 0; u < kRowKeys; ++u) {
+      const int i = k0 + u * kpw + lane / gs;
+      in[u] = i < hi;
+      ku[u] = vu[u] = make_uint4(0, 0, 0, 0);
+      if (in[u] && col) {
+        const int64_t key = keys.at(g, i);
+        ku[u] = *reinterpret_cast<const uint4*>(kp + key * a.ks.token);
+        vu[u] = *reinterpret_cast<const uint4*>(vp + key * a.vs.token);
+      }
+    }
+    float s[kRowKeys][RT];
+#pragma unroll
+    for (int u = 0; u < kRowKeys; ++u) {
+      float kf[8];
+      Elem<T>::open(ku[u], kf);
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        float d = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d = fmaf(q[r][i], kf[i], d);
+        for (int o = gs >> 1; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+        s[u][r] = in[u] ? d : -INFINITY;
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      float mx = m[r];
+#pragma unroll
+      for (int u = 0; u < kRowKeys; ++u) mx = fmaxf(mx, s[u][r]);
+      const float base = mx == -INFINITY ? 0.f : mx, f = ex2(m[r] - base);
+      m[r] = mx;
+      l[r] *= f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[r][i] *= f;
+#pragma unroll
+      for (int u = 0; u < kRowKeys; ++u) {
+        s[u][r] = ex2(s[u][r] - base);
+        l[r] += s[u][r];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kRowKeys; ++u) {
+      float vf[8];
+      Elem<T>::open(vu[u], vf);
+#pragma unroll
+      for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[r][i] = fmaf(s[u][r], vf[i], acc[r][i]);
+    }
+  }
+  // the groups of a warp
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    for (int o = gs; o < 32; o <<= 1) {
+      const float mo = __shfl_xor_sync(0xffffffffu, m[r], o), mx = fmaxf(m[r], mo), base = mx == -INFINITY ? 0.f : mx;
+      const float f = ex2(m[r] - base), fo = ex2(mo - base);
+      l[r] = l[r] * f + __shfl_xor_sync(0xffffffffu, l[r], o) * fo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[r][i] = acc[r][i] * f + __shfl_xor_sync(0xffffffffu, acc[r][i], o) * fo;
+      m[r] = mx;
+    }
+  }
+  float* sm = smem + kRowWarps * RT * a.D;
+  float* sl = sm + kRowWarps * RT;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    if (lane < gs && col)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) smem[(warp * RT + r) * a.D + at * 8 + i] = acc[r][i];
+    if (lane == 0) {
+      sm[warp * RT + r] = m[r];
+      sl[warp * RT + r] = l[r];
+    }
+  }
+  __syncthreads();
+  // eight values of a row to a thread
+  for (int e = threadIdx.x; e < RT * (a.D / 8); e += kRowWarps * 32) {
+    const int r = e / (a.D / 8), c = e % (a.D / 8) * 8;
+    const int64_t row = (int64_t)chunk * RT + r;
+    const int t = (int)(row / R), h = j * R + (int)(row % R);
+    if (t >= a.Q) continue;
+    float mx = -INFINITY, sum = 0.f, out[8] = {};
+#pragma unroll
+    for (int w = 0; w < kRowWarps; ++w) mx = fmaxf(mx, sm[w * RT + r]);
+    const float base = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+    for (int w = 0; w < kRowWarps; ++w) {
+      const float f = ex2(sm[w * RT + r] - base);
+      sum = fmaf(sl[w * RT + r], f, sum);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) out[i] = fmaf(smem[(w * RT + r) * a.D + c + i], f, out[i]);
+    }
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] *= inv;
+    const float l2 = mx == -INFINITY ? -INFINITY : mx + log2f(sum);
+    const int64_t at_row = ((int64_t)n * a.Q + t) * a.H + h;
+    if (splits > 1) {
+      float4* o = reinterpret_cast<float4*>(po + (at_row * splits + blockIdx.y) * a.D + c);
+      o[0] = make_float4(out[0], out[1], out[2], out[3]);
+      o[1] = make_float4(out[4], out[5], out[6], out[7]);
+      if (c == 0) pl[at_row * splits + blockIdx.y] = l2;
+    } else {
+      *reinterpret_cast<uint4*>((T*)a.o + n * a.os.item + t * a.os.token + h * a.os.head + c) = Elem<T>::pack(out);
+      if (c == 0 && a.lse) a.lse[at_row] = l2 * kLn2;
+    }
+  }
+}
+
+// The parts of the keys joined: eight values of a row to a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) k_attn_join(AttnArgs a, int splits, const float* __restrict__ po,
+                                                  const float* __restrict__ pl) {
+  pdl_wait();
+  pdl_trigger();
+  const int pieces = a.D / 8;
+  const int64_t rows = (int64_t)items_of(a.count, a.N) * a.Q * a.H;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows * pieces; e += (int64_t)gridDim.x * 256) {
+    const int64_t row = e / pieces;
+    const int c = (int)(e % pieces) * 8, h = (int)(row % a.H);
+    const int64_t nt = row / a.H;
+    const float* lp = pl + row * splits;
+    float mx = -INFINITY, sum = 0.f, out[8] = {};
+    for (int s = 0; s < splits; ++s) mx = fmaxf(mx, lp[s]);
+    const float base = mx == -INFINITY ? 0.f : mx;
+    for (int s = 0; s < splits; ++s) {
+      const float f = ex2(lp[s] - base);
+      const float4* o = reinterpret_cast<const float4*>(po + (row * splits + s) * a.D + c);
+      const float4 u = o[0], w = o[1];
+      sum += f;
+      out[0] = fmaf(u.x, f, out[0]);
+      out[1] = fmaf(u.y, f, out[1]);
+      out[2] = fmaf(u.z, f, out[2]);
+      out[3] = fmaf(u.w, f, out[3]);
+      out[4] = fmaf(w.x, f, out[4]);
+      out[5] = fmaf(w.y, f, out[5]);
+      out[6] = fmaf(w.z, f, out[6]);
+      out[7] = fmaf(w.w, f, out[7]);
+    }
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) out[i] *= inv;
+    *reinterpret_cast<uint4*>((T*)a.o + nt / a.Q * a.os.item + nt % a.Q * a.os.token + h * a.os.head + c) = Elem<T>::pack(out);
+    if (c == 0 && a.lse) a.lse[row] = mx == -INFINITY ? -INFINITY : (mx + log2f(sum)) * kLn2;
+  }
+}
+
+// How a call is split, and its workspace.
+struct Plan {
+  int rt, chunks, splits, gs;
+  size_t n, list, po, pl, total;
+};
+Plan plan(const AttnArgs& a) {
+  Plan p{};
+  const int64_t rows = (int64_t)a.Q * (a.H / a.J);
+  p.rt = rows > 1 ? 4 : 1;
+  p.chunks = (int)((rows + p.rt - 1) / p.rt);
+  for (p.gs = 1; p.gs * 8 < a.D;) p.gs <<= 1;
+  const int64_t ctas = (int64_t)a.N * a.J * p.chunks;
+  const int64_t want = (608 + ctas - 1) / ctas, most = (a.K + 255) / 256;
+  p.splits = (int)(want < most ? want : most);
+  if (p.splits < 1) p.splits = 1;
+  size_t o = 0;
+  auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, kAlign); return at; };
+  if (a.mask) {
+    p.n = take((size_t)a.G * 4);
+    p.list = take((size_t)a.G * a.K * 4);
+  }
+  if (p.splits > 1) {
+    const size_t all = (size_t)a.N * a.Q * a.H * p.splits;
+    p.po = take(all * a.D * 4);
+    p.pl = take(all * 4);
+  }
+  p.total = o;
+  return p;
+}
+
+template <typename T>
+cudaError_t run(const AttnArgs& a, cudaStream_t st) {
+  const Plan p = plan(a);
+  Keys keys{a.K, a.len, nullptr, nullptr};
+  cudaError_t e = cudaSuccess;
+  if (a.mask) {
+    int32_t* n = reinterpret_cast<int32_t*>(a.ws + p.n);
+    int32_t* list = reinterpret_cast<int32_t*>(a.ws + p.list);
+    e = launch_attn_keys(a, n, list, st);
+    if (e != cudaSuccess) return e;
+    keys.n = n;
+    keys.list = list;
+  }
+  float* po = reinterpret_cast<float*>(a.ws + p.po);
+  float* pl = reinterpret_cast<float*>(a.ws + p.pl);
+  const dim3 grid((unsigned)((int64_t)a.N * a.J * p.chunks), p.splits);
+  const size_t smem = (size_t)kRowWarps * p.rt * (a.D + 2) * 4;
+  e = launch_ex(p.rt == 1 ? k_attn_rows<T, 1> : k_attn_rows<T, 4>, grid, dim3(kRowWarps * 32), smem, st, 0, a, keys, p.gs,
+                p.chunks, p.splits, po, pl);
+  if (e != cudaSuccess || p.splits == 1) return e;
+  const int64_t pieces = (int64_t)a.N * a.Q * a.H * (a.D / 8), ctas = (pieces + 255) / 256;
+  return launch_ex(k_attn_join<T>, dim3((unsigned)(ctas < 1216 ? ctas : 1216)), dim3(256), 0, st, 0, a, p.splits,
+                   (const float*)po, (const float*)pl);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_keys(const AttnArgs& a, int32_t* n, int32_t* list, cudaStream_t st) {
+  return launch_ex(k_attn_keys, dim3(a.G), dim3(kListThreads), 0, st, 0, a.mask, a.mask_stride, a.len, a.K, n, list);
+}
+
+size_t attn_workspace(const AttnArgs& a) { return plan(a).total; }
+
+cudaError_t launch_attn(const AttnArgs& a, cudaStream_t st) {
+  return a.dtype == 1 ? run<__half>(a, st) : run<__nv_bfloat16>(a, st);
+}
+
+cudaError_t attn_status(int32_t** out) {
+  static std::atomic<int32_t*> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const bool keep = dev >= 0 && dev < 64;
+  *out = keep ? known[dev].load(std::memory_order_relaxed) : nullptr;
+  if (*out) return cudaSuccess;
+  void* p = nullptr;
+  e = cudaGetSymbolAddress(&p, g_status);
+  *out = static_cast<int32_t*>(p);
+  if (e == cudaSuccess && keep) known[dev].store(*out, std::memory_order_relaxed);
+  return e;
+}
+
+}  // namespace pa

@@ -1,0 +1,529 @@
+// Layer norm over the last axis, forward and backward.
+//
+//   y  = (x - mu) r w + b,  mu = mean x,  r = 1 / sqrt(mean (x - mu)^2 + eps)
+//   dx = r (g - mean g - xh mean(g xh)),  g = dy w,  xh = (x - mu) r
+//   dw = sum over rows of dy xh,  db = sum over rows of dy
+//
+// All of it is bound by memory: forward reads x and writes y, backward reads dy
+// and x and writes dx, 4 to 6 flops a byte. So a row is read once, 16 bytes per
+// load, and stays in registers for the variance (the two-pass form, so a large
+// mean costs no precision) and for the output; w and b stay in registers over
+// all rows of a thread; the next row is on its way while one is worked on.
+// Sums are fp32.
+//
+// A row belongs to a group of 4 to 32 lanes (a power of two) up to 8 16-byte
+// pieces a lane (backward 4 pieces of 16-bit values: the sums take registers
+// too), to a CTA up to 16 values a thread, beyond that it is read from memory in
+// each pass. dw and db: each thread sums its columns over its rows in
+// registers, the groups of a CTA are added in a fixed order, and a second kernel
+// adds the CTAs' sums in order: the result does not depend on timing.
+#include "pa_layers.h"
+
+namespace pa {
+namespace {
+
+constexpr int kThreads = 256;       // of the kernels with several rows per CTA
+constexpr int kMaxParts = 608;      // CTAs of the backward kernels: rows of partial sums (152 SMs x 4)
+constexpr int kCtaVals = 16;        // values a thread where a CTA has a row
+constexpr int kCtaThreads = 512;    // ... its threads at most
+
+// `V` values of a row: one 16-byte load where V > 1.
+template <typename T, int V>
+struct Piece;
+template <typename T>
+struct Piece<T, 1> {
+  using Raw = T;
+  __device__ static Raw load(const T* p) { return *p; }
+  __device__ static void store(T* p, const float* f) { *p = Elem<T>::put(f[0]); }
+  __device__ static void open(Raw r, float* f) { f[0] = Elem<T>::get(r); }
+  __device__ static Raw zero() { return Elem<T>::put(0.f); }
+};
+template <typename T, int V>
+struct Piece {
+  using Raw = uint4;
+  __device__ static Raw load(const T* p) { return *reinterpret_cast<const uint4*>(p); }
+  __device__ static void store(T* p, const float* f) { *reinterpret_cast<uint4*>(p) = Elem<T>::pack(f); }
+  __device__ static void open(Raw r, float* f) { Elem<T>::open(r, f); }
+  __device__ static Raw zero() { return make_uint4(0, 0, 0, 0); }
+};
+
+__device__ __forceinline__ int64_t counted(int64_t rows, const int32_t* count, int64_t per) {
+  if (!count) return rows;
+  const int64_t n = *count;
+  return n <= 0 ? 0 : n >= rows / per ? rows : n * per;  // rows is a multiple of per
+}
+
+// Sum over the threads that share a row: `tpr` lanes, or the CTA.
+template <bool CTA>
+struct RowSum {
+  float* s;  // CTA: one float per warp, two sets used in turn
+  int tpr, turn;
+  __device__ RowSum(float* sm, int t) : s(sm), tpr(t), turn(0) {}
+  __device__ float operator()(float v) {
+    if constexpr (!CTA) {
+      for (int o = tpr >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      return v;
+    } else {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      float* t = s + (turn ^= 1) * 32;  // the other set may still be read
+      if ((threadIdx.x & 31) == 0) t[threadIdx.x >> 5] = v;
+      __syncthreads();
+      const int nw = (blockDim.x + 31) >> 5;
+      float sum = 0.f;
+      for (int i = 0; i < nw; ++i) sum += t[i];
+      return sum;
+    }
+  }
+};
+
+// Which rows a thread works on, and its place in them.
+template <bool CTA>
+struct Rows {
+  int64_t first, step, lead;  // own first row; rows between turns; the warp's (CTA's) first row
+  int at;                     // place among the threads of a row
+  __device__ Rows(int tpr) {
+    if constexpr (CTA) {
+      first = lead = blockIdx.x;
+      step = gridDim.x;
+      at = threadIdx.x;
+    } else {
+      const int per_warp = 32 / tpr, lane = threadIdx.x & 31;
+      lead = ((int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5)) * per_warp;
+      first = lead + lane / tpr;
+      step = (int64_t)gridDim.x * (blockDim.x >> 5) * per_warp;
+      at = lane & (tpr - 1);
+    }
+  }
+};
+
+template <typename T, int V, int N, bool CTA>
+__global__ void __launch_bounds__(CTA ? kCtaThreads : kThreads) k_norm(const T* __restrict__ x, int64_t xs, const T* __restrict__ w,
+                                                               const T* __restrict__ b, float eps, T* y, int64_t ys,
+                                                               float* mean, float* rstd, int64_t rows, int cols, int tpr,
+                                                               const int32_t* count, int64_t per) {
+  using P = Piece<T, V>;
+  __shared__ float s_sum[64];
+  const Rows<CTA> R(tpr);
+  RowSum<CTA> sum(s_sum, tpr);
+  typename P::Raw wv[N], bv[N], cur[N];
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = counted(rows, count, per);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (R.at + i * tpr) * V;
+    wv[i] = w && c < cols ? P::load(w + c) : P::zero();
+    bv[i] = b && c < cols ? P::load(b + c) : P::zero();
+  }
+  auto fetch = [&](int64_t r) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (R.at + i * tpr) * V;
+      cur[i] = r < n && c < cols ? P::load(x + r * xs + c) : P::zero();
+    }
+  };
+  const float inv = 1.f / (float)cols;
+  int64_t r = R.first;
+  fetch(r);
+  for (int64_t lead = R.lead; lead < n; lead += R.step, r += R.step) {
+    float v[N * V], s = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      P::open(cur[i], v + i * V);
+#pragma unroll
+      for (int k = 0; k < V; ++k) s += v[i * V + k];
+    }
+    fetch(r + R.step);
+    const float mu = sum(s) * inv;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if ((R.at + i * tpr) * V < cols) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          v[i * V + k] -= mu;
+          s = fmaf(v[i * V + k], v[i * V + k], s);
+        }
+      }
+    const float rs = rsqrtf(sum(s) * inv + eps);
+    if (r < n) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = (R.at + i * tpr) * V;
+        if (c < cols) {
+          float o[V], wf[V], bf[V];
+          P::open(wv[i], wf);
+          P::open(bv[i], bf);
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            const float xh = v[i * V + k] * rs;
+            o[k] = w ? fmaf(xh, wf[k], bf[k]) : xh + bf[k];
+          }
+          P::store(y + r * ys + c, o);
+        }
+      }
+      if (mean && R.at == 0) {
+        mean[r] = mu;
+        rstd[r] = rs;
+      }
+    }
+  }
+}
+
+// Backward, and a CTA's sums of dw and db (part: [CTA][2][cols]) where SUMS.
+template <typename T, int V, int N, bool CTA, bool SUMS>
+__global__ void __launch_bounds__(CTA ? kCtaThreads : kThreads)
+    k_norm_bwd(const T* dy, int64_t dys, const T* x, int64_t xs, const T* __restrict__ w, const float* __restrict__ mean,
+               const float* __restrict__ rstd, T* dx, int64_t dxs, int64_t rows, int cols, int tpr, const int32_t* count,
+               int64_t per, float* __restrict__ part) {
+  using P = Piece<T, V>;
+  __shared__ float s_sum[64];
+  extern __shared__ float s_part[];  // [2][cols]
+  const Rows<CTA> R(tpr);
+  RowSum<CTA> sum(s_sum, tpr);
+  typename P::Raw wv[N], xc[N], yc[N];
+  float dw[SUMS ? N * V : 1] = {}, db[SUMS ? N * V : 1] = {};
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = counted(rows, count, per);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (R.at + i * tpr) * V;
+    wv[i] = w && c < cols ? P::load(w + c) : P::zero();
+  }
+  float mu_n = 0.f, rs_n = 0.f;
+  auto fetch = [&](int64_t r) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (R.at + i * tpr) * V;
+      const bool there = r < n && c < cols;
+      xc[i] = there ? P::load(x + r * xs + c) : P::zero();
+      yc[i] = there ? P::load(dy + r * dys + c) : P::zero();
+    }
+    if (r < n) {
+      mu_n = mean[r];
+      rs_n = rstd[r];
+    }
+  };
+  const float inv = 1.f / (float)cols;
+  int64_t r = R.first;
+  fetch(r);
+  for (int64_t lead = R.lead; lead < n; lead += R.step, r += R.step) {
+    float xh[N * V], g[N * V], s1 = 0.f, s2 = 0.f;
+    const float mu = mu_n, rs = rs_n;
+    const bool own = r < n;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float wf[V];
+      P::open(xc[i], xh + i * V);
+      P::open(yc[i], g + i * V);
+      P::open(wv[i], wf);
+      const bool there = own && (R.at + i * tpr) * V < cols;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int q = i * V + k;
+        xh[q] = there ? (xh[q] - mu) * rs : 0.f;
+        if constexpr (SUMS) {
+          dw[q] = fmaf(g[q], xh[q], dw[q]);
+          db[q] += g[q];
+        }
+        g[q] = w ? g[q] * wf[k] : g[q];
+        s1 += g[q];
+        s2 = fmaf(g[q], xh[q], s2);
+      }
+    }
+    fetch(r + R.step);
+    s1 = sum(s1) * inv;
+    s2 = sum(s2) * inv;
+    if (own) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = (R.at + i * tpr) * V;
+        if (c < cols) {
+          float o[V];
+#pragma unroll
+          for (int k = 0; k < V; ++k) o[k] = rs * (g[i * V + k] - s1 - xh[i * V + k] * s2);
+          P::store(dx + r * dxs + c, o);
+        }
+      }
+    }
+  }
+  if constexpr (SUMS) {
+    if constexpr (!CTA) {
+      // the groups of a warp, then the warps one after another
+      for (int o = tpr; o < 32; o <<= 1) {
+#pragma unroll
+        for (int q = 0; q < N * V; ++q) {
+          dw[q] += __shfl_xor_sync(0xffffffffu, dw[q], o);
+          db[q] += __shfl_xor_sync(0xffffffffu, db[q], o);
+        }
+      }
+      const int warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+      for (int t = 0; t < nw; ++t) {
+        if (warp == t && (int)(threadIdx.x & 31) < tpr) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const int c = (R.at + i * tpr) * V;
+            if (c < cols) {
+#pragma unroll
+              for (int k = 0; k < V; ++k) {
+                s_part[c + k] = dw[i * V + k] + (t ? s_part[c + k] : 0.f);
+                s_part[cols + c + k] = db[i * V + k] + (t ? s_part[cols + c + k] : 0.f);
+              }
+            }
+          }
+        }
+        __syncthreads();
+      }
+      float* o = part + (int64_t)blockIdx.x * 2 * cols;
+      for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) o[c] = s_part[c];
+    } else {
+      float* o = part + (int64_t)blockIdx.x * 2 * cols;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = (R.at + i * tpr) * V;
+        if (c < cols) {
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            o[c + k] = dw[i * V + k];
+            o[cols + c + k] = db[i * V + k];
+          }
+        }
+      }
+    }
+  }
+}
+
+// dw and db: the CTAs' sums added in order, 32 columns a CTA, eight threads a
+// column.
+template <typename T>
+__global__ void __launch_bounds__(256) k_norm_sums(const float* __restrict__ part, int parts, int cols, T* dw, T* db) {
+  __shared__ float s[8][33];
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
+  const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+  float v = 0.f;
+  if (c < 2 * (int64_t)cols) {
+    const int lo = (int)((int64_t)parts * g / 8), hi = (int)((int64_t)parts * (g + 1) / 8);
+#pragma unroll 4
+    for (int p = lo; p < hi; ++p) v += __ldcg(part + (int64_t)p * 2 * cols + c);
+  }
+  s[g][lane] = v;
+  __syncthreads();
+  if (g == 0 && c < 2 * (int64_t)cols) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) v += s[i][lane];
+    T* o = c < cols ? dw : db;
+    if (o) o[c < cols ? c : c - cols] = Elem<T>::put(v);
+  }
+}
+
+// Rows of any length: a CTA per row, every pass reads it again.
+template <typename T>
+__global__ void __launch_bounds__(1024) k_norm_long(const T* x, int64_t xs, const T* __restrict__ w, const T* __restrict__ b,
+                                                   float eps, T* y, int64_t ys, float* mean, float* rstd, int64_t rows,
+                                                   int cols, const int32_t* count, int64_t per) {
+  __shared__ float s_sum[64];
+  RowSum<true> sum(s_sum, 0);
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = counted(rows, count, per);
+  const float inv = 1.f / (float)cols;
+  for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
+    const T* p = x + r * xs;
+    float s = 0.f;
+    for (int c = threadIdx.x; c < cols; c += blockDim.x) s += Elem<T>::get(p[c]);
+    const float mu = sum(s) * inv;
+    s = 0.f;
+    for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+      const float v = Elem<T>::get(p[c]) - mu;
+      s = fmaf(v, v, s);
+    }
+    const float rs = rsqrtf(sum(s) * inv + eps);
+    for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+      const float xh = (Elem<T>::get(p[c]) - mu) * rs, bf = b ? Elem<T>::get(b[c]) : 0.f;
+      y[r * ys + c] = Elem<T>::put(w ? fmaf(xh, Elem<T>::get(w[c]), bf) : xh + bf);
+    }
+    if (mean && threadIdx.x == 0) {
+      mean[r] = mu;
+      rstd[r] = rs;
+    }
+  }
+}
+template <typename T>
+__global__ void __launch_bounds__(1024) k_norm_long_bwd(const T* dy, int64_t dys, const T* x, int64_t xs,
+                                                       const T* __restrict__ w, const float* __restrict__ mean,
+                                                       const float* __restrict__ rstd, T* dx, int64_t dxs, int64_t rows,
+                                                       int cols, const int32_t* count, int64_t per) {
+  __shared__ float s_sum[64];
+  RowSum<true> sum(s_sum, 0);
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = counted(rows, count, per);
+  const float inv = 1.f / (float)cols;
+  for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
+    const float mu = mean[r], rs = rstd[r];
+    float s1 = 0.f, s2 = 0.f;
+    for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+      const float g = Elem<T>::get(dy[r * dys + c]) * (w ? Elem<T>::get(w[c]) : 1.f);
+      s1 += g;
+      s2 = fmaf(g, (Elem<T>::get(x[r * xs + c]) - mu) * rs, s2);
+    }
+    s1 = sum(s1) * inv;
+    s2 = sum(s2) * inv;
+    for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+      const float g = Elem<T>::get(dy[r * dys + c]) * (w ? Elem<T>::get(w[c]) : 1.f);
+      const float xh = (Elem<T>::get(x[r * xs + c]) - mu) * rs;
+      dx[r * dxs + c] = Elem<T>::put(rs * (g - s1 - xh * s2));
+    }
+  }
+}
+// ... and its sums of dw and db: a thread has a column of a part of the rows.
+// Before the kernel above, which may write dx over dy or x.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_norm_long_sums(const T* dy, int64_t dys, const T* x, int64_t xs,
+                                                            const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                            int64_t rows, int cols, const int32_t* count, int64_t per,
+                                                            float* __restrict__ part) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = counted(rows, count, per);
+  const int64_t lo = n * blockIdx.y / gridDim.y, hi = n * (blockIdx.y + 1) / gridDim.y;
+  const int c = blockIdx.x * kThreads + threadIdx.x;
+  if (c >= cols) return;
+  float dw = 0.f, db = 0.f;
+#pragma unroll 4
+  for (int64_t r = lo; r < hi; ++r) {
+    const float g = Elem<T>::get(dy[r * dys + c]);
+    dw = fmaf(g, (Elem<T>::get(x[r * xs + c]) - mean[r]) * rstd[r], dw);
+    db += g;
+  }
+  part[(int64_t)blockIdx.y * 2 * cols + c] = dw;
+  part[(int64_t)blockIdx.y * 2 * cols + cols + c] = db;
+}
+
+// How a row is shared: `tpr` threads, n pieces each, of V values.
+struct Form {
+  int tpr, n;
+  bool vec, cta;  // n = 0: rows too long for registers
+};
+Form form_of(int cols, int vec, bool aligned, int most) {
+  if (aligned) {
+    const int pieces = cols / vec;
+    if (pieces <= 32 * most) {  // fewest idle lanes; of those the most pieces a lane
+      Form best{32, most, true, false};
+      int waste = 1 << 30;
+      for (int n : {5, 4, 3, 2, 1, 8}) {
+        if (n > most) continue;
+        int t = 4;
+        while (t < 32 && t * n < pieces) t <<= 1;
+        if (t * n >= pieces && t * n - pieces < waste) best = {t, n, true, false}, waste = t * n - pieces;
+      }
+      return best;
+    }
+    const int n = kCtaVals / vec, t = ((pieces + n - 1) / n + 31) / 32 * 32;
+    if (t <= kCtaThreads) return {t, n, true, true};
+  } else {
+    if (cols <= 64) return {32, 2, false, false};
+    if (cols <= 256) return {32, 8, false, false};
+    const int t = ((cols + kCtaVals - 1) / kCtaVals + 31) / 32 * 32;
+    if (t <= kCtaThreads) return {t, kCtaVals, false, true};
+  }
+  return {0, 0, false, true};
+}
+
+bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <typename T, int V, int N, bool CTA>
+cudaError_t forward(const NormArgs& a, const Form& f, cudaStream_t st) {
+  const int64_t per_cta = CTA ? 1 : kThreads / f.tpr;
+  const int64_t want = (a.rows + per_cta - 1) / per_cta;
+  const int64_t most = 152 * (CTA ? 1024 / f.tpr : 4);
+  return launch_ex(k_norm<T, V, N, CTA>, dim3((unsigned)(want < most ? want : most)), dim3(CTA ? f.tpr : kThreads), 0, st, 0,
+                   (const T*)a.x, a.xs, (const T*)a.w, (const T*)a.b, a.eps, (T*)a.y, a.ys, a.mean, a.rstd, a.rows, a.cols,
+                   f.tpr, a.count, a.per);
+}
+template <typename T, int V, int N, bool CTA>
+cudaError_t backward(const NormArgs& a, const Form& f, int* parts, cudaStream_t st) {
+  if constexpr (!CTA && V == 8 && N > 4) return cudaErrorNotSupported;  // form_of has no such form
+  else {
+  const int64_t per_cta = CTA ? 1 : kThreads / f.tpr;
+  const int64_t want = (a.rows + per_cta - 1) / per_cta;
+  const int most = CTA ? 152 * (f.tpr > 256 ? 1 : 2) : kMaxParts;
+  const int grid = (int)(want < most ? want : most);
+  *parts = grid;
+  const size_t smem = CTA ? 0 : (size_t)2 * a.cols * sizeof(float);
+  auto go = [&](auto kern, size_t sm) {
+    return launch_ex(kern, dim3(grid), dim3(CTA ? f.tpr : kThreads), sm, st, 0, (const T*)a.dy, a.dys, (const T*)a.x, a.xs,
+                     (const T*)a.w, (const float*)a.mean, (const float*)a.rstd, (T*)a.dx, a.dxs, a.rows, a.cols, f.tpr,
+                     a.count, a.per, a.part);
+  };
+  return a.part ? go(k_norm_bwd<T, V, N, CTA, true>, smem) : go(k_norm_bwd<T, V, N, CTA, false>, 0);
+  }
+}
+
+template <typename T>
+cudaError_t run(const NormArgs& a, bool back, cudaStream_t st) {
+  constexpr int V = Elem<T>::kVec;
+  bool aligned = a.cols % V == 0 && a.xs % V == 0 && on16(a.x) && on16(a.w);
+  aligned = aligned && (back ? a.dys % V == 0 && a.dxs % V == 0 && on16(a.dy) && on16(a.dx) : a.ys % V == 0 && on16(a.y) && on16(a.b));
+  const Form f = form_of(a.cols, V, aligned, back && V == 8 ? 4 : 8);
+  int parts = 0;
+  cudaError_t e = cudaSuccess;
+#define PA_NORM_CASE(VV, NN, CC) e = back ? backward<T, VV, NN, CC>(a, f, &parts, st) : forward<T, VV, NN, CC>(a, f, st)
+  if (f.n == 0) {
+    const dim3 grid((unsigned)(a.rows < 304 ? a.rows : 304));
+    if (!back)
+      return launch_ex(k_norm_long<T>, grid, dim3(1024), 0, st, 0, (const T*)a.x, a.xs, (const T*)a.w, (const T*)a.b, a.eps,
+                       (T*)a.y, a.ys, a.mean, a.rstd, a.rows, a.cols, a.count, a.per);
+    if (a.part) {
+      parts = norm_parts(a.rows) < 64 ? norm_parts(a.rows) : 64;
+      e = launch_ex(k_norm_long_sums<T>, dim3((a.cols + kThreads - 1) / kThreads, parts), dim3(kThreads), 0, st, 0,
+                    (const T*)a.dy, a.dys, (const T*)a.x, a.xs, (const float*)a.mean, (const float*)a.rstd, a.rows, a.cols,
+                    a.count, a.per, a.part);
+    }
+    if (e == cudaSuccess)
+      e = launch_ex(k_norm_long_bwd<T>, grid, dim3(1024), 0, st, 0, (const T*)a.dy, a.dys, (const T*)a.x, a.xs, (const T*)a.w,
+                    (const float*)a.mean, (const float*)a.rstd, (T*)a.dx, a.dxs, a.rows, a.cols, a.count, a.per);
+  } else if (f.vec && f.cta) {
+    PA_NORM_CASE(V, kCtaVals / V, true);
+  } else if (f.vec) {
+    switch (f.n) {
+      case 1: PA_NORM_CASE(V, 1, false); break;
+      case 2: PA_NORM_CASE(V, 2, false); break;
+      case 3: PA_NORM_CASE(V, 3, false); break;
+      case 4: PA_NORM_CASE(V, 4, false); break;
+      case 5: PA_NORM_CASE(V, 5, false); break;
+      default: PA_NORM_CASE(V, 8, false); break;
+    }
+  } else if (f.cta) {
+    PA_NORM_CASE(1, kCtaVals, true);
+  } else if (f.n == 2) {
+    PA_NORM_CASE(1, 2, false);
+  } else {
+    PA_NORM_CASE(1, 8, false);
+  }
+#undef PA_NORM_CASE
+  if (e != cudaSuccess || !back || !a.part) return e;
+  return launch_ex(k_norm_sums<T>, dim3((unsigned)((2 * (int64_t)a.cols + 31) / 32)), dim3(256), 0, st, 0,
+                   (const float*)a.part, parts, a.cols, (T*)a.dw, (T*)a.db);
+}
+
+cudaError_t dispatch(const NormArgs& a, bool back, cudaStream_t st) {
+  switch (a.dtype) {
+    case 0: return run<float>(a, back, st);
+    case 1: return run<__half>(a, back, st);
+    default: return run<__nv_bfloat16>(a, back, st);
+  }
+}
+
+}  // namespace
+
+int norm_parts(int64_t rows) { return rows < kMaxParts ? (int)rows : kMaxParts; }
+
+cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) { return dispatch(a, false, st); }
+cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t st) { return dispatch(a, true, st); }
+
+}  // namespace pa

@@ -1,0 +1,247 @@
+// Host side of the layer operators' C ABI: argument checks and dispatch. The
+// calls keep no state; what a kernel's launch needs is in its arguments.
+#include <cmath>
+#include <cstdio>
+#include <string>
+
+#include "../../include/paraanya.h"
+#include "pa_layers.h"
+
+namespace pa {
+void set_error(const std::string& msg);
+}
+
+namespace {
+
+pa_status fail(pa_status s, const char* where, const char* what) {
+  char buf[256];
+  std::snprintf(buf, sizeof buf, "%s: %s", where, what);
+  pa::set_error(buf);
+  return s;
+}
+pa_status arg(const char* where, const char* what) { return fail(PA_ERR_ARG, where, what); }
+pa_status done(const char* where, cudaError_t e) {
+  return e == cudaSuccess ? PA_OK : fail(PA_ERR_CUDA, where, cudaGetErrorString(e));
+}
+bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+// A workspace of at least `need` bytes.
+pa_status workspace_ok(const char* where, const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return PA_OK;
+  if (!ws || !aligned(ws, pa::kAlign)) return fail(PA_ERR_WORKSPACE, where, "workspace is NULL or not 256-byte aligned");
+  if (bytes < need) return fail(PA_ERR_WORKSPACE, where, "workspace too small");
+  return PA_OK;
+}
+
+constexpr int64_t kMaxRows = (int64_t)1 << 40;
+
+pa_status norm_ok(const char* where, const pa::NormArgs& a, double eps) {
+  if (a.dtype < PA_F32 || a.dtype > PA_BF16) return arg(where, "dtype must be PA_F32, PA_F16 or PA_BF16");
+  if (a.rows < 0 || a.rows > kMaxRows || a.cols < 1) return arg(where, "need rows >= 0 and cols >= 1");
+  if (!(eps >= 0.0) || !std::isfinite(eps)) return arg(where, "eps must be finite and >= 0");
+  if (a.count && (a.per < 1 || a.rows % a.per != 0))
+    return arg(where, "rows must be a multiple of rows_per_item (>= 1)");
+  const uintptr_t e = a.dtype == PA_F32 ? 4 : 2;
+  for (const void* p : {a.x, a.w, a.b, (const void*)a.y, a.dy, (const void*)a.dx, (const void*)a.dw, (const void*)a.db})
+    if (!aligned(p, e)) return arg(where, "a tensor is not aligned to its elements");
+  if (a.rows > 1 && (a.xs < a.cols || (a.y && a.ys < a.cols) || (a.dy && a.dys < a.cols) || (a.dx && a.dxs < a.cols)))
+    return arg(where, "row strides must be at least cols");
+  return PA_OK;
+}
+
+pa_status attn_ok(const char* where, const pa_attention_t* t, pa::AttnArgs* a) {
+  if (!t) return arg(where, "NULL arguments");
+  if (t->dtype != PA_F16 && t->dtype != PA_BF16) return arg(where, "dtype must be PA_F16 or PA_BF16");
+  if (t->items < 0 || t->tokens < 0 || t->sources < 0 || t->keys < 0) return arg(where, "sizes must be >= 0");
+  if (t->heads < 1 || t->kv_heads < 1 || t->heads % t->kv_heads != 0) return arg(where, "kv_heads must divide heads");
+  if (t->heads > 65535) return arg(where, "at most 65535 heads");
+  if (t->head_dim < 8 || t->head_dim > 256 || t->head_dim % 8 != 0)
+    return arg(where, "head_dim must be a multiple of 8, 8 to 256");
+  // rows and units are counted in 32 bits below the strides
+  if ((int64_t)t->tokens * t->heads >= (int64_t)1 << 31 || (int64_t)t->items * t->heads >= (int64_t)1 << 31)
+    return arg(where, "tokens * heads and items * heads must be below 2^31");
+  if ((double)t->items * t->tokens * t->heads >= 1.6e10 || (double)t->sources * t->keys * t->kv_heads >= 1.6e10)
+    return arg(where, "too many rows");
+  a->dtype = t->dtype;
+  a->N = t->items;
+  a->Q = t->tokens;
+  a->G = t->sources;
+  a->K = t->keys;
+  a->H = t->heads;
+  a->J = t->kv_heads;
+  a->D = t->head_dim;
+  a->scale = (float)t->scale;
+  a->q = t->q;
+  a->k = t->k;
+  a->v = t->v;
+  a->o = t->out;
+  a->lse = t->lse;
+  a->src = t->source;
+  a->src_stride = t->source_stride;
+  a->len = t->lengths;
+  a->mask = t->mask;
+  a->mask_stride = t->mask_stride;
+  a->count = t->n_items_dev;
+  a->dout = t->dout;
+  a->dq = t->dq;
+  a->dk = t->dk;
+  a->dv = t->dv;
+  const auto st = [](const int64_t* s) { return pa::Strides{s[0], s[1], s[2]}; };
+  a->qs = st(t->q_stride);
+  a->ks = st(t->k_stride);
+  a->vs = st(t->v_stride);
+  a->os = st(t->out_stride);
+  a->dos = st(t->dout_stride);
+  a->dqs = st(t->dq_stride);
+  a->dks = st(t->dk_stride);
+  a->dvs = st(t->dv_stride);
+  return PA_OK;
+}
+
+// A tensor of the attention: there if it has values, 16-byte rows.
+const char* tensor_bad(const void* p, const int64_t* s, int64_t values) {
+  if (values > 0 && !p) return "a tensor is NULL";
+  if (!aligned(p, 16)) return "a tensor is not 16-byte aligned";
+  for (int i = 0; i < 3; ++i)
+    if (s[i] % 8 != 0) return "strides must be multiples of 8 elements";
+  return nullptr;
+}
+
+pa_status attn_call(const char* where, const pa_attention_t* t, bool back, void* ws, size_t bytes, void* stream) {
+  pa::AttnArgs a{};
+  pa_status s = attn_ok(where, t, &a);
+  if (s != PA_OK) return s;
+  if (!std::isfinite(t->scale) || !(a.scale > 0.f) || !std::isfinite(a.scale * 1.5f))
+    return arg(where, "scale must be finite and > 0");
+  if (!a.src && a.G < a.N) return arg(where, "without source there must be as many sources as items");
+  const int64_t rows = (int64_t)a.N * a.Q, states = (int64_t)a.G * a.K;
+  const char* bad = tensor_bad(a.q, t->q_stride, rows);
+  if (!bad) bad = tensor_bad(a.k, t->k_stride, states);
+  if (!bad) bad = tensor_bad(a.v, t->v_stride, states);
+  if (!bad) bad = tensor_bad(a.o, t->out_stride, rows);
+  if (!bad && back) {
+    bad = tensor_bad(a.dout, t->dout_stride, rows);
+    if (!bad) bad = tensor_bad(a.dq, t->dq_stride, rows);
+    if (!bad) bad = tensor_bad(a.dk, t->dk_stride, states);
+    if (!bad) bad = tensor_bad(a.dv, t->dv_stride, states);
+    if (!bad && rows > 0 && !a.lse) bad = "lse is NULL";
+  }
+  if (bad) return arg(where, bad);
+  s = workspace_ok(where, ws, bytes, back ? pa::attn_backward_workspace(a) : pa::attn_workspace(a));
+  if (s != PA_OK) return s;
+  if (rows == 0 && (!back || states == 0)) return PA_OK;
+  a.ws = static_cast<unsigned char*>(ws);
+  cudaError_t e = pa::attn_status(&a.status);
+  if (e == cudaSuccess) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    e = back ? pa::launch_attn_backward(a, st) : pa::launch_attn(a, st);
+  }
+  return done(where, e);
+}
+
+}  // namespace
+
+extern "C" {
+
+pa_status pa_layer_norm(int dtype, int64_t rows, int cols, const void* x, int64_t x_stride, const void* weight,
+                        const void* bias, double eps, void* y, int64_t y_stride, float* mean, float* rstd,
+                        const int32_t* n_items_dev, int64_t rows_per_item, void* stream) {
+  const char* where = "pa_layer_norm";
+  pa::NormArgs a{};
+  a.dtype = dtype;
+  a.rows = rows;
+  a.cols = cols;
+  a.x = x;
+  a.xs = x_stride;
+  a.w = weight;
+  a.b = bias;
+  a.eps = (float)eps;
+  a.y = y;
+  a.ys = y_stride;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.count = n_items_dev;
+  a.per = rows_per_item;
+  const pa_status s = norm_ok(where, a, eps);
+  if (s != PA_OK) return s;
+  if (!mean != !rstd) return arg(where, "mean and rstd go together");
+  if (rows == 0) return PA_OK;
+  if (!x || !y) return arg(where, "x or y is NULL");
+  return done(where, pa::launch_norm(a, static_cast<cudaStream_t>(stream)));
+}
+
+size_t pa_layer_norm_backward_workspace_bytes(int64_t rows, int cols) {
+  if (rows < 0 || rows > kMaxRows || cols < 1) return 0;
+  return pa::align_up((size_t)(pa::norm_parts(rows) + 1) * 2 * cols * sizeof(float), pa::kAlign);
+}
+
+pa_status pa_layer_norm_backward(int dtype, int64_t rows, int cols, const void* dy, int64_t dy_stride, const void* x,
+                                 int64_t x_stride, const void* weight, const float* mean, const float* rstd, void* dx,
+                                 int64_t dx_stride, void* dweight, void* dbias, const int32_t* n_items_dev,
+                                 int64_t rows_per_item, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  const char* where = "pa_layer_norm_backward";
+  pa::NormArgs a{};
+  a.dtype = dtype;
+  a.rows = rows;
+  a.cols = cols;
+  a.x = x;
+  a.xs = x_stride;
+  a.w = weight;
+  a.mean = const_cast<float*>(mean);
+  a.rstd = const_cast<float*>(rstd);
+  a.count = n_items_dev;
+  a.per = rows_per_item;
+  a.dy = dy;
+  a.dys = dy_stride;
+  a.dx = dx;
+  a.dxs = dx_stride;
+  a.dw = dweight;
+  a.db = dbias;
+  pa_status s = norm_ok(where, a, 0.0);
+  if (s != PA_OK) return s;
+  if (rows > 0 && (!x || !dy || !dx || !mean || !rstd)) return arg(where, "x, dy, dx, mean or rstd is NULL");
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (dweight || dbias) {
+    s = workspace_ok(where, workspace_dev, workspace_bytes, pa_layer_norm_backward_workspace_bytes(rows, cols));
+    if (s != PA_OK) return s;
+    a.part = static_cast<float*>(workspace_dev);
+    if (rows == 0) {
+      const size_t bytes = (size_t)cols * (dtype == PA_F32 ? 4 : 2);
+      cudaError_t e = dweight ? cudaMemsetAsync(dweight, 0, bytes, st) : cudaSuccess;
+      if (e == cudaSuccess && dbias) e = cudaMemsetAsync(dbias, 0, bytes, st);
+      return done(where, e);
+    }
+  }
+  if (rows == 0) return PA_OK;
+  return done(where, pa::launch_norm_backward(a, st));
+}
+
+size_t pa_attention_workspace_bytes(const pa_attention_t* t, int backward) {
+  pa::AttnArgs a{};
+  if (attn_ok("pa_attention_workspace_bytes", t, &a) != PA_OK) return (size_t)-1;
+  return backward ? pa::attn_backward_workspace(a) : pa::attn_workspace(a);
+}
+
+pa_status pa_attention(const pa_attention_t* a, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  return attn_call("pa_attention", a, false, workspace_dev, workspace_bytes, stream);
+}
+
+pa_status pa_attention_backward(const pa_attention_t* a, void* workspace_dev, size_t workspace_bytes, void* stream) {
+  return attn_call("pa_attention_backward", a, true, workspace_dev, workspace_bytes, stream);
+}
+
+pa_status pa_attention_check(void* stream) {
+  const char* where = "pa_attention_check";
+  int32_t *word = nullptr, got = 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = pa::attn_status(&word);
+  if (e == cudaSuccess) e = cudaMemcpyAsync(&got, word, sizeof got, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, sizeof got, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return done(where, e);
+  if (got == pa::kDevOk) return PA_OK;
+  if (got == pa::kDevTimeout) return fail(PA_ERR_TIMEOUT, where, "a device-side bounded wait ran out");
+  return fail(PA_ERR_DEVICE, where, "a source index was out of range");
+}
+
+}  // extern "C"

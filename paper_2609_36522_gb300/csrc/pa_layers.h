@@ -1,0 +1,140 @@
+// Shared by the layer operators' entry points (pa_layers.cpp) and kernels
+// (k_norm.cu, k_attn*.cu): element types, argument blocks, launchers.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "pa_internal.h"
+
+namespace pa {
+
+// ---- element types: 16 bytes at a time, arithmetic in fp32 ----------------
+template <typename T>
+struct Elem;
+template <>
+struct Elem<float> {
+  static constexpr int kVec = 4;
+  __device__ static float get(float v) { return v; }
+  __device__ static float put(float v) { return v; }
+  __device__ static void open(uint4 q, float* f) {
+    f[0] = __uint_as_float(q.x);
+    f[1] = __uint_as_float(q.y);
+    f[2] = __uint_as_float(q.z);
+    f[3] = __uint_as_float(q.w);
+  }
+  __device__ static uint4 pack(const float* f) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+};
+template <>
+struct Elem<__half> {
+  static constexpr int kVec = 8;
+  __device__ static float get(__half v) { return __half2float(v); }
+  __device__ static __half put(float v) { return __float2half_rn(v); }
+  __device__ static uint32_t pack2(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  __device__ static float2 open2(uint32_t q) { return __half22float2(*reinterpret_cast<const __half2*>(&q)); }
+  __device__ static void open(uint4 q, float* f) {
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = open2(u[i]);
+      f[2 * i] = v.x;
+      f[2 * i + 1] = v.y;
+    }
+  }
+  __device__ static uint4 pack(const float* f) {
+    return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+  }
+};
+template <>
+struct Elem<__nv_bfloat16> {
+  static constexpr int kVec = 8;
+  __device__ static float get(__nv_bfloat16 v) { return __bfloat162float(v); }
+  __device__ static __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
+  __device__ static uint32_t pack2(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  __device__ static float2 open2(uint32_t q) {
+    return make_float2(__uint_as_float(q << 16), __uint_as_float(q & 0xffff0000u));
+  }
+  __device__ static void open(uint4 q, float* f) {
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = open2(u[i]);
+      f[2 * i] = v.x;
+      f[2 * i + 1] = v.y;
+    }
+  }
+  __device__ static uint4 pack(const float* f) {
+    return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+  }
+};
+
+// ---- layer norm -------------------------------------------------------------
+struct NormArgs {
+  int dtype;
+  int64_t rows;
+  int cols;
+  const void* x;
+  int64_t xs;             // elements from a row to the next
+  const void *w, *b;      // NULL: ones, zeros
+  float eps;
+  void* y;
+  int64_t ys;
+  float *mean, *rstd;     // written forward (NULL: not kept), read backward
+  const int32_t* count;   // device: the first *count groups of `per` rows count (NULL: all rows)
+  int64_t per;
+  // backward
+  const void* dy;
+  int64_t dys;
+  void* dx;
+  int64_t dxs;
+  void *dw, *db;
+  float* part;            // partial sums of dw and db
+};
+int norm_parts(int64_t rows);  // rows of partial sums that launch_norm_backward may write, each 2 * cols floats
+cudaError_t launch_norm(const NormArgs& a, cudaStream_t st);
+cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t st);
+
+// ---- cross attention ----------------------------------------------------------
+// Item, token and head strides in elements; the last axis is contiguous.
+struct Strides {
+  int64_t item, token, head;
+};
+struct AttnArgs {
+  int dtype;                       // 1: float16, 2: bfloat16
+  int N, Q, G, K, H, J, D;         // items, tokens, sources, keys, heads, heads of k and v, head size
+  float scale;
+  const void *q, *k, *v;
+  void* o;
+  float* lse;                      // [N][Q][H], NULL: not kept
+  Strides qs, ks, vs, os;          // item of k and v: a source
+  const int32_t* src;              // device: item n attends to source src[n * src_stride] (NULL: n)
+  int64_t src_stride;
+  const int32_t* len;              // device [G]: only keys before it count (NULL: all)
+  const uint8_t* mask;             // device [G][mask_stride]: zero: the key does not count (NULL: all do)
+  int64_t mask_stride;
+  const int32_t* count;            // device: only items before it count (NULL: all)
+  int32_t* status;                 // device: first failure
+  // backward
+  const void* dout;
+  void *dq, *dk, *dv;
+  Strides dos, dqs, dks, dvs;
+  unsigned char* ws;
+};
+size_t attn_workspace(const AttnArgs& a);
+size_t attn_backward_workspace(const AttnArgs& a);
+cudaError_t launch_attn(const AttnArgs& a, cudaStream_t st);
+cudaError_t launch_attn_backward(const AttnArgs& a, cudaStream_t st);
+// The device's status word (k_attn.cu).
+cudaError_t attn_status(int32_t** out);
+
+}  // namespace pa
