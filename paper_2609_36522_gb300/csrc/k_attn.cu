@@ -237,8 +237,13 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a, int splits, const
   }
 }
 
+// Up to this many query rows of an item and key head the CUDA cores take them:
+// a tile of the tensor-core kernel has 128.
+constexpr int kRowsMost = 16;
+
 // How a call is split, and its workspace.
 struct Plan {
+  bool tc;
   int rt, chunks, splits, gs;
   size_t n, list, po, pl, total;
 };
@@ -252,6 +257,8 @@ Plan plan(const AttnArgs& a) {
   const int64_t want = (608 + ctas - 1) / ctas, most = (a.K + 255) / 256;
   p.splits = (int)(want < most ? want : most);
   if (p.splits < 1) p.splits = 1;
+  p.tc = rows > kRowsMost;
+  if (p.tc) p.splits = attn_tc_splits(a);
   size_t o = 0;
   auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, kAlign); return at; };
   if (a.mask) {
@@ -284,7 +291,7 @@ cudaError_t run(const AttnArgs& a, cudaStream_t st) {
   float* pl = reinterpret_cast<float*>(a.ws + p.pl);
   const dim3 grid((unsigned)((int64_t)a.N * a.J * p.chunks), p.splits);
   const size_t smem = (size_t)kRowWarps * p.rt * (a.D + 2) * 4;
-  e = launch_ex(p.rt == 1 ? k_attn_rows<T, 1> : k_attn_rows<T, 4>, grid, dim3(kRowWarps * 32), smem, st, 0, a, keys, p.gs,
+  e = p.tc ? launch_attn_tc(a, keys, po, pl, st) : launch_ex(p.rt == 1 ? k_attn_rows<T, 1> : k_attn_rows<T, 4>, grid, dim3(kRowWarps * 32), smem, st, 0, a, keys, p.gs,
                 p.chunks, p.splits, po, pl);
   if (e != cudaSuccess || p.splits == 1) return e;
   const int64_t pieces = (int64_t)a.N * a.Q * a.H * (a.D / 8), ctas = (pieces + 255) / 256;

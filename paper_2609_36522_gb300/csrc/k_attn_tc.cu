@@ -1,0 +1,530 @@
+// Cross attention, forward, on the tensor cores (tcgen05).
+//
+// A tile is 128 query rows of one item and key head (tokens, and the heads that
+// share the key head). A work item is NWG such tiles that go over the same keys, one
+// tile per group of four softmax warps: a thread has a row. Per tile of `kt` keys
+//   S = Q K^T        (both operands in shared memory, S in TMEM)
+//   P = exp2(c S - c m), c = scale log2 e, m the running maximum of the row
+//   O += P V         (P written over S in TMEM as the A operand, V as it lies)
+// One thread issues the MMAs of all groups in turn, so while one group's MMAs run
+// the others do their exponentials; a group hands P over and goes on to the next
+// S. O stays in TMEM; it is rescaled only where a row's maximum grows by more than
+// 2^8 (probabilities stay below 2^8, which both 16-bit types hold). The last O of a
+// work item is read only after the next one's P is written, so no group waits for
+// its MMAs there.
+//
+// Three loader warps copy Q, K and V with 16-byte asynchronous copies, ahead of use;
+// keys are picked from the list of those that count. Where all keys are one tile and the next
+// work item has the same ones (rows of one trajectory), K and V stay in shared
+// memory: CTAs take work items in turn, heads innermost, so that a CTA keeps its
+// head while neighbouring CTAs read the other heads of the same tokens.
+//
+// The row sums are fp32 sums of the unrounded probabilities; P enters the second
+// product in the tensors' 16-bit type.
+#include "pa_attn.cuh"
+
+namespace pa {
+namespace {
+
+constexpr int kTable = 256;  // work items of a CTA whose source and keys are looked up at the start
+
+struct TcShape {
+  int kt, d16, stages, qbufs, splits;
+  int tiles, groups;  // query tiles of an item and key head; groups of NWG of them
+  uint32_t tmem;      // columns allocated
+};
+
+__host__ __device__ inline int stage_units(int D) { return D / 8 < 8 ? D / 8 : 8; }  // 16-byte units of a staged row
+
+template <int NWG>
+__host__ __device__ constexpr int tc_threads() {
+  return NWG * 128 + kLoadThreads + 32;
+}
+
+template <typename T, int NWG>
+__global__ void __launch_bounds__(tc_threads<NWG>(), 1)
+    k_attn_tc(AttnArgs a, Keys keys, TcShape sh, float* __restrict__ po, float* __restrict__ pl) {
+  constexpr int kBf16 = Elem<T>::kBf16;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[NWG],
+      p_full[NWG], o_full[NWG];
+  __shared__ uint32_t s_taddr;
+  __shared__ int2 s_work[kTable];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
+  const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2;
+  unsigned char* sq = smem;
+  unsigned char* sk = sq + sh.qbufs * NWG * qtile;
+  unsigned char* sv = sk + sh.stages * ktile;
+  unsigned char* so = sv + sh.stages * ktile;
+  if (tid == 0) {
+    for (int b = 0; b < 2; ++b) {
+      for (int g = 0; g < NWG; ++g) mbar_init(&q_full[b][g], kLoadThreads);
+      mbar_init(&q_empty[b], 1);
+      mbar_init(&k_full[b], kLoadThreads);
+      mbar_init(&k_empty[b], 1);
+      mbar_init(&v_full[b], kLoadThreads);
+      mbar_init(&v_empty[b], 1);
+    }
+    for (int g = 0; g < NWG; ++g) {
+      mbar_init(&s_full[g], 1);
+      mbar_init(&p_full[g], 4);
+      mbar_init(&o_full[g], 1);
+    }
+    fence_barrier_init();
+  }
+  if (D & 8) {  // the columns beyond D, once: no copy touches them
+    const int rows = sh.qbufs * NWG * 128 + 2 * sh.stages * kt;
+    for (int r = tid; r < rows; r += tc_threads<NWG>())
+      *reinterpret_cast<uint4*>(smem + (uint32_t)(r >> 3) * d16 * 16 + (d16 / 8 - 1) * 128 + (r & 7) * 16) =
+          make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  if (warp == 0) {
+    tmem_alloc(&s_taddr, sh.tmem);
+    tc_fence_before_sync();
+  }
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t taddr = s_taddr;
+  pdl_wait();
+  pdl_trigger();
+  const int works = items_of(a.count, a.N) * sh.groups * a.J * sh.splits;
+
+  // ---- work items: item n, key head j, group of tiles, part of the keys
+  struct Work {
+    int n, j, group, part, g, lo, cnt;
+  };
+  auto look = [&](int w) {  // source and number of keys that count
+    const int n = w / (sh.splits * a.J * sh.groups);
+    const int g = source_of(a.src, a.src_stride, n, a.G, a.status);
+    return make_int2(g, g < 0 ? 0 : keys.count(g));
+  };
+  for (int i = tid; i < kTable; i += tc_threads<NWG>()) {
+    const int64_t w = blockIdx.x + (int64_t)i * gridDim.x;
+    if (w < works) s_work[i] = look((int)w);
+  }
+  __syncthreads();
+  auto work = [&](int i, int w) {
+    Work k;
+    const int2 f = i < kTable ? s_work[i] : look(w);
+    k.g = f.x;
+    k.part = sh.splits > 1 ? w % sh.splits : 0;
+    w /= sh.splits;
+    k.j = w % a.J;
+    w /= a.J;
+    k.group = w % sh.groups;
+    k.n = w / sh.groups;
+    if (sh.splits > 1) {
+      const int tiles = (f.y + kt - 1) / kt, t0 = tiles * k.part / sh.splits, t1 = tiles * (k.part + 1) / sh.splits;
+      k.lo = t0 * kt;
+      k.cnt = min(f.y, t1 * kt) - k.lo;
+    } else {
+      k.lo = 0;
+      k.cnt = f.y;
+    }
+    return k;
+  };
+  bool bad = false;
+
+  if (warp < 4 * NWG) {
+    // ================= softmax: a thread per row =================
+    const int g = warp >> 2;
+    const uint32_t tS = taddr + (uint32_t)g * (kt + d16) + ((uint32_t)(warp & 3) << 21), tO = tS + kt;
+    const float c2 = a.scale * kLog2e;
+    const int su = stage_units(D), sstride = su | 1;
+    const uint32_t usu = 65536u / su + 1;
+    unsigned char* stage = so + warp * 32 * sstride * 16;
+    uint32_t s_par = 0, o_par = 0;
+    struct Pending {
+      int64_t off, row;  // this thread's row: in out (elements), among all rows; negative: none
+      int part;
+      float m, l;
+      bool any;
+    } pend;
+    pend.any = false;
+    // O / l of a work item to out
+    auto finish = [&](const Pending& f, bool empty) {
+      const float inv = empty ? 0.f : 1.f / f.l;
+      if (!empty) {
+        wait_or_bad(&o_full[g], o_par, bad, a.status);
+        o_par ^= 1;
+        __syncwarp();
+        tc_fence_after_sync();
+      }
+      const float scale = bad ? __int_as_float(0x7fffffff) : inv;
+      if (sh.splits > 1) {
+        float* o = po + (f.row * sh.splits + f.part) * D;
+        for (int c = 0; c < d16; c += 16) {
+          uint32_t r[16] = {};
+          if (!empty) {
+            tmem_ld(tO + c, r);
+            tmem_ld_wait();
+          }
+          if (f.row >= 0) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              if (c + 4 * q < D)
+                *reinterpret_cast<float4*>(o + c + 4 * q) =
+                    make_float4(__uint_as_float(r[4 * q]) * scale, __uint_as_float(r[4 * q + 1]) * scale,
+                                __uint_as_float(r[4 * q + 2]) * scale, __uint_as_float(r[4 * q + 3]) * scale);
+          }
+        }
+        if (f.row >= 0) pl[f.row * sh.splits + f.part] = empty ? -INFINITY : f.m * c2 + log2f(f.l);
+        return;
+      }
+      if (f.row >= 0 && a.lse) a.lse[f.row] = empty ? -INFINITY : (f.m * c2 + log2f(f.l)) * kLn2;
+      for (int c0 = 0; c0 < D; c0 += su * 8) {
+        for (int c = c0; c < min(c0 + su * 8, D); c += 16) {
+          uint32_t r[16] = {};
+          if (!empty) {
+            tmem_ld(tO + c, r);
+            tmem_ld_wait();
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (h && c + 8 >= D) break;
+            float v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(r[8 * h + q]) * scale;
+            *reinterpret_cast<uint4*>(stage + (lane * sstride + (c - c0) / 8 + h) * 16) = Elem<T>::pack(v);
+          }
+        }
+        __syncwarp();
+        const int units = min(su, (D - c0) / 8);  // the rows' pieces, neighbouring lanes on neighbouring pieces
+        for (int q = 0; q < su; ++q) {
+          const uint32_t e = q * 32 + lane, row = (e * usu) >> 16, u = e - row * su;
+          const int64_t off = __shfl_sync(0xffffffffu, f.off, row);
+          if (off >= 0 && (int)u < units)
+            *reinterpret_cast<uint4*>((T*)a.o + off + c0 + u * 8) =
+                *reinterpret_cast<const uint4*>(stage + (row * sstride + u) * 16);
+        }
+        __syncwarp();
+      }
+    };
+    for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
+      const Work k = work(i, w);
+      const int tile = k.group * NWG + g;
+      if (tile >= sh.tiles) continue;
+      Pending cur;
+      {
+        const uint32_t m = (uint32_t)tile * 128 + (warp & 3) * 32 + lane;
+        const uint32_t t = R == 1 ? m : m / (uint32_t)R, h = k.j * R + (R == 1 ? 0 : m - t * R);
+        const bool there = t < (uint32_t)a.Q;
+        cur.off = there ? k.n * a.os.item + t * a.os.token + h * a.os.head : -1;
+        cur.row = there ? ((int64_t)k.n * a.Q + t) * a.H + h : -1;
+        cur.part = k.part;
+        cur.any = true;
+      }
+      if (k.cnt <= 0) {
+        finish(cur, true);
+        continue;
+      }
+      cur.m = -INFINITY;
+      cur.l = 0.f;
+      for (int k0 = 0; k0 < k.cnt; k0 += kt) {
+        const int n = min(kt, k.cnt - k0), n16 = (n + 15) & ~15;
+        wait_or_bad(&s_full[g], s_par, bad, a.status);
+        s_par ^= 1;
+        __syncwarp();
+        tc_fence_after_sync();
+        // the tile's maximum
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        int c = 0;
+        for (; c + 32 <= n16; c += 32) {
+          uint32_t r[32];
+          tmem_ld(tS + c, r);
+          tmem_ld_wait();
+          if (c + 32 <= n) {
+#pragma unroll
+            for (int q = 0; q < 32; ++q) mx[q & 3] = fmaxf(mx[q & 3], __uint_as_float(r[q]));
+          } else {
+#pragma unroll
+            for (int q = 0; q < 32; ++q) mx[q & 3] = fmaxf(mx[q & 3], c + q < n ? __uint_as_float(r[q]) : -INFINITY);
+          }
+        }
+        if (c < n16) {
+          uint32_t r[16];
+          tmem_ld(tS + c, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int q = 0; q < 16; ++q) mx[q & 3] = fmaxf(mx[q & 3], c + q < n ? __uint_as_float(r[q]) : -INFINITY);
+        }
+        const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        if (k0 == 0) {
+          cur.m = m;
+        } else {
+          const bool grow = (m - cur.m) * c2 > 8.f;
+          if (__any_sync(0xffffffffu, grow)) {  // the MMAs before this S are complete: O may be changed
+            const float f = grow ? ex2((cur.m - m) * c2) : 1.f;
+            if (grow) cur.m = m;
+            cur.l *= f;
+            for (int o = 0; o < d16; o += 16) {
+              uint32_t r[16];
+              tmem_ld(tO + o, r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int q = 0; q < 16; ++q) r[q] = __float_as_uint(__uint_as_float(r[q]) * f);
+              tmem_st(tO + o, r);
+            }
+          }
+        }
+        const float mc = cur.m == -INFINITY ? 0.f : cur.m * c2;
+        float sum[4] = {};
+        auto probs = [&](auto& r, auto& p, int c, bool whole) {
+          constexpr int W = sizeof(r) / 4;
+#pragma unroll
+          for (int q = 0; q < W; q += 2) {
+            float x = ex2(fmaf(__uint_as_float(r[q]), c2, -mc)), y = ex2(fmaf(__uint_as_float(r[q + 1]), c2, -mc));
+            if (!whole) {
+              x = c + q < n ? x : 0.f;
+              y = c + q + 1 < n ? y : 0.f;
+            }
+            sum[q & 2] += x;
+            sum[(q & 2) + 1] += y;
+            p[q / 2] = Elem<T>::pack2(x, y);
+          }
+        };
+        c = 0;
+        for (; c + 32 <= n16; c += 32) {
+          uint32_t r[32], p[16];
+          tmem_ld(tS + c, r);
+          tmem_ld_wait();
+          if (c + 32 <= n) probs(r, p, c, true);
+          else probs(r, p, c, false);
+          tmem_st(tS + c / 2, p);
+        }
+        if (c < n16) {
+          uint32_t r[16], p[8];
+          tmem_ld(tS + c, r);
+          tmem_ld_wait();
+          probs(r, p, c, false);
+          tmem_st(tS + c / 2, p);
+        }
+        cur.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        if (k0 == 0 && pend.any) finish(pend, false);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[g]);
+      }
+      pend = cur;
+    }
+    if (pend.any) finish(pend, false);
+  } else if (warp < 4 * NWG + kLoadWarps) {
+    // ================= loads =================
+    const int lt = tid - 4 * NWG * 32;
+    Jobs jobs;
+    uint32_t it = 0, qi = 0;  // key tiles and work items so far
+    int hg = -1, hj = 0, hlo = 0, hcnt = 0;  // the keys that stay
+    for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
+      const Work k = work(i, w);
+      if (k.cnt <= 0) continue;
+      const bool reuse = hg == k.g && hj == k.j && hlo == k.lo && hcnt == k.cnt;
+      hg = k.cnt <= kt ? k.g : -1;
+      hj = k.j;
+      hlo = k.lo;
+      hcnt = k.cnt;
+      const T* kp = (const T*)a.k + k.g * a.ks.item + k.j * a.ks.head;
+      const T* vp = (const T*)a.v + k.g * a.vs.item + k.j * a.vs.head;
+      auto key_tile = [&](const T* base, int64_t step, unsigned char* to, int k0) {
+        const int n = min(kt, k.cnt - k0);
+        copy_tile<T>(smem_u32(to), (n + 15) & ~15, D, d16, base, lt, [&](int r) {
+          return r < n ? base + keys.at(k.g, k.lo + k0 + r) * step : (const T*)nullptr;
+        });
+      };
+      const uint32_t qb = qi % sh.qbufs;
+      for (int k0 = 0; k0 < k.cnt; k0 += kt) {
+        uint32_t st = it % sh.stages;
+        if (!reuse) {
+          if (it >= (uint32_t)sh.stages) jobs.wait(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
+          key_tile(kp, a.ks.token, sk + st * ktile, k0);
+          jobs.push(&k_full[st]);
+        }
+        if (k0 == 0) {
+          if (qi >= (uint32_t)sh.qbufs) jobs.wait(&q_empty[qb], (qi / sh.qbufs - 1) & 1u, bad, a.status);
+          const T* qp = (const T*)a.q + k.n * a.qs.item + k.j * R * a.qs.head;
+#pragma unroll 1
+          for (int g = 0; g < NWG; ++g) {
+            const int tile = k.group * NWG + g;
+            if (tile < sh.tiles) {
+              const uint32_t m0 = (uint32_t)tile * 128;
+              copy_tile<T>(smem_u32(sq + (qb * NWG + g) * qtile), 128, D, d16, qp, lt, [&](int r) {
+                const uint32_t m = m0 + r, t = R == 1 ? m : m / (uint32_t)R;
+                return t < (uint32_t)a.Q ? qp + t * a.qs.token + (R == 1 ? 0 : (m - t * R) * a.qs.head) : (const T*)nullptr;
+              });
+            }
+            jobs.push(&q_full[qb][g]);
+          }
+        }
+        if (!reuse) {
+          if (it >= (uint32_t)sh.stages) jobs.wait(&v_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
+          key_tile(vp, a.vs.token, sv + st * ktile, k0);
+          jobs.push(&v_full[st]);
+          ++it;
+        }
+      }
+      ++qi;
+    }
+    jobs.flush();
+  } else if (lane == 0) {
+    // ================= MMAs =================
+    const uint32_t aq = smem_u32(sq), ak = smem_u32(sk), av = smem_u32(sv), step = (uint32_t)d16 * 32;  // 16 rows
+    uint32_t it = 0, qi = 0, p_par = 0;  // p_par: a bit per group
+    int hg = -1, hj = 0, hlo = 0, hcnt = 0;
+    // the step whose O += P V are still to come
+    bool pv[NWG], v_ready = true, plast = false, pfirst = false, have = false;
+#pragma unroll
+    for (int g = 0; g < NWG; ++g) pv[g] = false;
+    uint32_t pst = 0, pit = 0;
+    int pn16 = 0;
+    auto second = [&](int g) {  // O += P V of the step before
+      wait_or_bad(&p_full[g], (p_par >> g) & 1u, bad, a.status);
+      p_par ^= 1u << g;
+      if (!v_ready) {
+        wait_or_bad(&v_full[pst], (pit / sh.stages) & 1u, bad, a.status);
+        v_ready = true;
+      }
+      tc_fence_after_sync();
+      const uint32_t tS = taddr + (uint32_t)g * (kt + d16), idesc = tc_idesc_16(128, d16, kBf16, 0, 1);
+      for (int ks = 0; ks < pn16 / 16; ++ks)
+        tc_mma_f16_ta(tS + kt, tS + ks * 8, tile_desc_cols(av + pst * ktile + ks * step, d16), idesc,
+                      !pfirst || ks > 0 ? 1u : 0u);
+      if (plast) tc_commit(&o_full[g]);
+    };
+    for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
+      const Work k = work(i, w);
+      if (k.cnt <= 0) continue;
+      const bool reuse = hg == k.g && hj == k.j && hlo == k.lo && hcnt == k.cnt;
+      const bool held = hg >= 0;
+      hg = k.cnt <= kt ? k.g : -1;
+      hj = k.j;
+      hlo = k.lo;
+      hcnt = k.cnt;
+      const uint32_t qb = qi % sh.qbufs;
+      for (int k0 = 0; k0 < k.cnt; k0 += kt) {
+        const int n16 = (min(kt, k.cnt - k0) + 15) & ~15;
+        uint32_t st = pst;
+        if (!reuse) {
+          if (k0 == 0 && held) tc_commit(&k_empty[pst]);  // the keys that stayed are used up
+          st = it % sh.stages;
+          wait_or_bad(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
+        }
+        const uint32_t idesc = tc_idesc_16(128, n16, kBf16, 0, 0);
+#pragma unroll
+        for (int g = 0; g < NWG; ++g) {
+          if (pv[g]) second(g);
+          pv[g] = k.group * NWG + g < sh.tiles;
+          if (pv[g]) {
+            if (k0 == 0) wait_or_bad(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+            tc_fence_after_sync();
+            const uint32_t tS = taddr + (uint32_t)g * (kt + d16);
+            for (int ks = 0; ks < d16 / 16; ++ks)
+              tc_mma_f16(tS, tile_desc_rows(aq + (qb * NWG + g) * qtile + ks * 256, d16),
+                         tile_desc_rows(ak + st * ktile + ks * 256, d16), idesc, ks > 0 ? 1u : 0u);
+            tc_commit(&s_full[g]);
+          }
+        }
+        if (have && !reuse) tc_commit(&v_empty[pst]);  // all of the step before is issued
+        if (k.cnt > kt) tc_commit(&k_empty[st]);
+        have = true;
+        if (!reuse) {
+          pit = it++;
+          v_ready = false;
+        }
+        pst = st;
+        pn16 = n16;
+        pfirst = k0 == 0;
+        plast = k0 + kt >= k.cnt;
+      }
+      tc_commit(&q_empty[qb]);
+      ++qi;
+    }
+#pragma unroll
+    for (int g = 0; g < NWG; ++g)
+      if (pv[g]) second(g);
+  }
+  __syncthreads();
+  __syncwarp();
+  if (warp == 0) tmem_dealloc(taddr, sh.tmem);
+}
+
+// ---- shapes -------------------------------------------------------------------
+struct TcPlan {
+  int nwg, grid;
+  TcShape sh;
+  size_t smem;
+};
+constexpr int kSms = 152;
+constexpr size_t kSmemMost = 224 << 10;
+
+size_t tc_smem(int nwg, const TcShape& sh, int D) {
+  const size_t row = (size_t)sh.d16 * 2;
+  return ((size_t)sh.qbufs * nwg * 128 + 2 * (size_t)sh.stages * sh.kt) * row +
+         (size_t)nwg * 128 * (stage_units(D) | 1) * 16;
+}
+
+TcPlan tc_plan(const AttnArgs& a) {
+  TcPlan p{};
+  TcShape& s = p.sh;
+  s.d16 = (a.D + 15) & ~15;
+  const int64_t rows = (int64_t)a.Q * (a.H / a.J);
+  s.tiles = (int)((rows + 127) / 128);
+  const int k16 = (a.K + 15) & ~15;
+  s.kt = k16 < 128 ? (k16 > 0 ? k16 : 16) : 128;
+  if (s.kt + s.d16 > 256 && s.d16 < 256) {  // two groups need narrower key tiles
+    const int kt = (256 - s.d16) & ~15;
+    if (kt >= 64) s.kt = kt;
+  }
+  p.nwg = 512 / (s.kt + s.d16);
+  if (p.nwg > 4) p.nwg = 4;
+  if (p.nwg > s.tiles) p.nwg = s.tiles;
+  s.qbufs = 2;
+  s.stages = 2;
+  while (tc_smem(p.nwg, s, a.D) > kSmemMost) {
+    if (s.qbufs == 2) s.qbufs = 1;
+    else if (s.kt > 64) s.kt -= 16;
+    else if (p.nwg > 1) --p.nwg;
+    else s.stages = 1;
+  }
+  s.groups = (s.tiles + p.nwg - 1) / p.nwg;
+  s.tmem = 32;
+  while (s.tmem < (uint32_t)(p.nwg * (s.kt + s.d16))) s.tmem <<= 1;
+  // too few work items for the SMs: the keys are split, joined afterwards
+  const int64_t works = (int64_t)a.N * s.groups * a.J, ktiles = (a.K + s.kt - 1) / s.kt;
+  s.splits = 1;
+  if (works > 0 && works * 2 <= kSms && ktiles > 1) {
+    const int64_t most = kSms / works;
+    s.splits = (int)(most < ktiles ? most : ktiles);
+  }
+  const int64_t all = works * s.splits;
+  p.grid = (int)(all < kSms ? all : kSms);
+  if (a.K <= s.kt && a.J < kSms && all > kSms) p.grid -= kSms % a.J;  // a CTA keeps its head
+  p.smem = tc_smem(p.nwg, s, a.D);
+  return p;
+}
+
+template <typename T, int NWG>
+cudaError_t go(const AttnArgs& a, const Keys& keys, const TcPlan& p, float* po, float* pl, cudaStream_t st) {
+  static SmemGranted granted;
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_tc<T, NWG>), p.smem, granted);
+  if (e != cudaSuccess) return e;
+  return launch_ex(k_attn_tc<T, NWG>, dim3(p.grid), dim3(tc_threads<NWG>()), p.smem, st, 0, a, keys, p.sh, po, pl);
+}
+
+}  // namespace
+
+int attn_tc_splits(const AttnArgs& a) { return tc_plan(a).sh.splits; }
+
+cudaError_t launch_attn_tc(const AttnArgs& a, const Keys& keys, float* po, float* pl, cudaStream_t st) {
+  const TcPlan p = tc_plan(a);
+  const bool half = a.dtype == 1;
+  switch (p.nwg) {
+    case 1: return half ? go<__half, 1>(a, keys, p, po, pl, st) : go<__nv_bfloat16, 1>(a, keys, p, po, pl, st);
+    case 2: return half ? go<__half, 2>(a, keys, p, po, pl, st) : go<__nv_bfloat16, 2>(a, keys, p, po, pl, st);
+    case 3: return half ? go<__half, 3>(a, keys, p, po, pl, st) : go<__nv_bfloat16, 3>(a, keys, p, po, pl, st);
+    default: return half ? go<__half, 4>(a, keys, p, po, pl, st) : go<__nv_bfloat16, 4>(a, keys, p, po, pl, st);
+  }
+}
+
+}  // namespace pa

@@ -31,7 +31,7 @@ struct Elem<float> {
 };
 template <>
 struct Elem<__half> {
-  static constexpr int kVec = 8;
+  static constexpr int kVec = 8, kBf16 = 0;
   __device__ static float get(__half v) { return __half2float(v); }
   __device__ static __half put(float v) { return __float2half_rn(v); }
   __device__ static uint32_t pack2(float a, float b) {
@@ -54,7 +54,7 @@ struct Elem<__half> {
 };
 template <>
 struct Elem<__nv_bfloat16> {
-  static constexpr int kVec = 8;
+  static constexpr int kVec = 8, kBf16 = 1;
   __device__ static float get(__nv_bfloat16 v) { return __bfloat162float(v); }
   __device__ static __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
   __device__ static uint32_t pack2(float a, float b) {
