@@ -10,11 +10,12 @@ namespace {
 __device__ int32_t g_status;
 
 // ---------------------------------------------------------------------------
-// The keys of each source that count, in order; a CTA per source.
+// The keys of each source that count, in order; a CTA per source. pos (may be
+// NULL): each key's place among them, -1 for the others.
 constexpr int kListThreads = 256;
 __global__ void __launch_bounds__(kListThreads) k_attn_keys(const uint8_t* __restrict__ mask, int64_t stride,
                                                            const int32_t* __restrict__ len, int K, int32_t* __restrict__ n,
-                                                           int32_t* __restrict__ list) {
+                                                           int32_t* __restrict__ list, int32_t* __restrict__ pos) {
   __shared__ int s_n[kListThreads / 32];
   pdl_wait();
   pdl_trigger();
@@ -22,7 +23,7 @@ __global__ void __launch_bounds__(kListThreads) k_attn_keys(const uint8_t* __res
   const int end = len ? min(max(len[g], 0), K) : K;
   const uint8_t* m = mask + g * stride;
   int base = 0;
-  for (int k0 = 0; k0 < end; k0 += kListThreads) {
+  for (int k0 = 0; k0 < (pos ? K : end); k0 += kListThreads) {
     const int k = k0 + threadIdx.x;
     const bool in = k < end && m[k] != 0;
     const unsigned b = __ballot_sync(0xffffffffu, in);
@@ -35,7 +36,9 @@ __global__ void __launch_bounds__(kListThreads) k_attn_keys(const uint8_t* __res
       if (w < warp) before += c;
       base += c;
     }
-    if (in) list[(int64_t)g * K + before + __popc(b & ((1u << lane) - 1))] = k;
+    before += __popc(b & ((1u << lane) - 1));
+    if (in) list[(int64_t)g * K + before] = k;
+    if (pos && k < K) pos[(int64_t)g * K + k] = in ? before : -1;
     __syncthreads();
   }
   if (threadIdx.x == 0) n[g] = base;
@@ -282,7 +285,7 @@ cudaError_t run(const AttnArgs& a, cudaStream_t st) {
   if (a.mask) {
     int32_t* n = reinterpret_cast<int32_t*>(a.ws + p.n);
     int32_t* list = reinterpret_cast<int32_t*>(a.ws + p.list);
-    e = launch_attn_keys(a, n, list, st);
+    e = launch_attn_keys(a, n, list, nullptr, st);
     if (e != cudaSuccess) return e;
     keys.n = n;
     keys.list = list;
@@ -301,8 +304,8 @@ cudaError_t run(const AttnArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_attn_keys(const AttnArgs& a, int32_t* n, int32_t* list, cudaStream_t st) {
-  return launch_ex(k_attn_keys, dim3(a.G), dim3(kListThreads), 0, st, 0, a.mask, a.mask_stride, a.len, a.K, n, list);
+cudaError_t launch_attn_keys(const AttnArgs& a, int32_t* n, int32_t* list, int32_t* pos, cudaStream_t st) {
+  return launch_ex(k_attn_keys, dim3(a.G), dim3(kListThreads), 0, st, 0, a.mask, a.mask_stride, a.len, a.K, n, list, pos);
 }
 
 size_t attn_workspace(const AttnArgs& a) { return plan(a).total; }

@@ -1,152 +1,756 @@
-// Cross attention, backward:
-//   p_ij = exp(s_ij - lse_i),  dp_ij = do_i . v_j,  delta_i = do_i . o_i,
+// Cross attention, backward, on the tensor cores:
+//   p_ij = exp(s_ij - lse_i),  dp_ij = do_i . v_j,  delta_i = sum_j p_ij dp_ij,
 //   ds_ij = p_ij (dp_ij - delta_i),
 //   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i,
 // the last two over all rows of all items of the source and all heads that share
 // the key head, always in the same order.
+//
+//   k_attn_dq   a tile of 128 query rows per group of softmax warps, as in the
+//               forward kernel, over the key tiles twice: once for delta, once for dq
+//               (where all keys are one tile, S and dP stay in TMEM between the two).
+//               delta = do . out would save the first pass, but out is
+//               rounded to 16 bits: with much of the weight on one key that error is most of
+//               ds (dq off by 6e-3 of its norm against 1.7e-3 for the rounding of dq itself).
+//   k_attn_dkv  a tile of 128 keys and a part of the source's query rows per CTA, the
+//               transposed products S^T = K Q^T and dP^T = V dO^T on 64 query rows at a
+//               time: P^T and dS^T are then A operands where they lie in TMEM, and
+//               dV += P^T dO, dK += dS^T Q add up in TMEM over all of the CTA's rows.
+//   k_attn_sum  the parts added in order, rounded, spread over the keys.
 #include "pa_attn.cuh"
 
 namespace pa {
 namespace {
 
-// dq: a warp per row; delta is kept for the kernel below. Lane groups as in the
-// forward kernel.
-template <typename T>
-__global__ void __launch_bounds__(256) k_attn_dq(AttnArgs a, Keys keys, int gs, float* __restrict__ delta) {
-  const int lane = threadIdx.x & 31, at = lane & (gs - 1), kpw = 32 / gs;
+constexpr int kSms = 152;
+constexpr size_t kSmemMost = 224 << 10;
+
+// Sources' items in order, by source: a CTA per source.
+constexpr int kOrderThreads = 256;
+__global__ void __launch_bounds__(kOrderThreads) k_attn_order(const int32_t* __restrict__ src, int64_t stride,
+                                                             const int32_t* __restrict__ count, int N,
+                                                             int32_t* __restrict__ first, int32_t* __restrict__ order) {
+  __shared__ int s_n[kOrderThreads / 32], s_less[kOrderThreads / 32];
   pdl_wait();
   pdl_trigger();
-  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int h = (int)(row % a.H);
-  const int64_t nt = row / a.H;
-  const int t = (int)(nt % a.Q);
-  const int64_t n = nt / a.Q;
-  if (n >= items_of(a.count, a.N)) return;
-  const int g = source_of(a.src, a.src_stride, (int)n, a.G, a.status);
-  const int kn = g < 0 ? 0 : keys.count(g), j = h / (a.H / a.J);
-  const bool col = at * 8 < a.D;
-  float q[8] = {}, d[8] = {}, o[8] = {}, acc[8] = {};
-  if (col) {
-    Elem<T>::open(*reinterpret_cast<const uint4*>((const T*)a.q + n * a.qs.item + t * a.qs.token + h * a.qs.head + at * 8), q);
-    Elem<T>::open(*reinterpret_cast<const uint4*>((const T*)a.dout + n * a.dos.item + t * a.dos.token + h * a.dos.head + at * 8), d);
-    Elem<T>::open(*reinterpret_cast<const uint4*>((const T*)a.o + n * a.os.item + t * a.os.token + h * a.os.head + at * 8), o);
+  const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, items = items_of(count, N);
+  int less = 0;
+  for (int n = threadIdx.x; n < items; n += kOrderThreads) {
+    const int s = src[n * stride];
+    less += s >= 0 && s < g;
   }
-  float dl = 0.f;
+  less = __reduce_add_sync(0xffffffffu, less);
+  if (lane == 0) s_less[warp] = less;
+  __syncthreads();
+  int base = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) dl = fmaf(d[i], o[i], dl);
-  for (int w = gs >> 1; w > 0; w >>= 1) dl += __shfl_xor_sync(0xffffffffu, dl, w);
-  if (lane == 0) delta[row] = dl;
-  const float c2 = a.scale * kLog2e, l2 = kn ? a.lse[row] * kLog2e : 0.f;
-  const T* kp = (const T*)a.k + (int64_t)max(g, 0) * a.ks.item + j * a.ks.head + at * 8;
-  const T* vp = (const T*)a.v + (int64_t)max(g, 0) * a.vs.item + j * a.vs.head + at * 8;
-  for (int k0 = 0; k0 < kn; k0 += kpw) {
-    const int i = k0 + lane / gs;
-    float kf[8] = {}, vf[8] = {}, s = 0.f, dp = 0.f;
-    if (i < kn && col) {
-      const int64_t key = keys.at(g, i);
-      Elem<T>::open(*reinterpret_cast<const uint4*>(kp + key * a.ks.token), kf);
-      Elem<T>::open(*reinterpret_cast<const uint4*>(vp + key * a.vs.token), vf);
-    }
+  for (int w = 0; w < kOrderThreads / 32; ++w) base += s_less[w];
+  if (threadIdx.x == 0) first[2 * g] = base;
+  for (int n0 = 0; n0 < items; n0 += kOrderThreads) {
+    const int n = n0 + threadIdx.x;
+    const bool in = n < items && src[n * stride] == g;
+    const unsigned b = __ballot_sync(0xffffffffu, in);
+    if (lane == 0) s_n[warp] = __popc(b);
+    __syncthreads();
+    int before = base;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      s = fmaf(q[e], kf[e], s);
-      dp = fmaf(d[e], vf[e], dp);
+    for (int w = 0; w < kOrderThreads / 32; ++w) {
+      const int c = s_n[w];
+      if (w < warp) before += c;
+      base += c;
     }
-    for (int w = gs >> 1; w > 0; w >>= 1) {
-      s += __shfl_xor_sync(0xffffffffu, s, w);
-      dp += __shfl_xor_sync(0xffffffffu, dp, w);
-    }
-    const float ds = i < kn ? ex2(s * c2 - l2) * (dp - dl) : 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = fmaf(ds, kf[e], acc[e]);
+    if (in) order[before + __popc(b & ((1u << lane) - 1))] = n;
+    __syncthreads();
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    for (int w = gs; w < 32; w <<= 1) acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], w);
-    acc[e] *= a.scale;
-  }
-  if (lane < gs && col)
-    *reinterpret_cast<uint4*>((T*)a.dq + n * a.dqs.item + t * a.dqs.token + h * a.dqs.head + at * 8) = Elem<T>::pack(acc);
+  if (threadIdx.x == 0) first[2 * g + 1] = base;
 }
 
-// dk and dv: a warp per key and key head, over all rows of the source in order.
-template <typename T>
-__global__ void __launch_bounds__(256) k_attn_dkv(AttnArgs a, Keys keys, int gs, const float* __restrict__ delta) {
-  const int lane = threadIdx.x & 31, at = lane & (gs - 1), rpw = 32 / gs, R = a.H / a.J;
-  pdl_wait();
-  pdl_trigger();
-  const int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (unit >= (int64_t)a.G * a.J * a.K) return;
-  const int j = (int)(unit % a.J), key = (int)(unit / a.J % a.K), g = (int)(unit / a.J / a.K);
-  const bool col = at * 8 < a.D;
-  const bool in = (!a.len || key < a.len[g]) && (!a.mask || a.mask[g * a.mask_stride + key] != 0);
-  float kf[8] = {}, vf[8] = {}, dk[8] = {}, dv[8] = {};
-  if (in && col) {
-    Elem<T>::open(*reinterpret_cast<const uint4*>((const T*)a.k + g * a.ks.item + key * a.ks.token + j * a.ks.head + at * 8), kf);
-    Elem<T>::open(*reinterpret_cast<const uint4*>((const T*)a.v + g * a.vs.item + key * a.vs.token + j * a.vs.head + at * 8), vf);
-  }
-  const float c2 = a.scale * kLog2e;
-  const int N = in ? items_of(a.count, a.N) : 0;
-  for (int64_t n = 0; n < N; ++n) {
-    if ((a.src ? a.src[n * a.src_stride] : n) != g) continue;
-    for (int r0 = 0; r0 < a.Q * R; r0 += rpw) {
-      const int r = r0 + lane / gs, t = r / R, h = j * R + r % R;
-      const bool there = t < a.Q;
-      float q[8] = {}, d[8] = {}, s = 0.f, dp = 0.f;
-      if (there && col) {
-        Elem<T>::open(*reinterpret_cast<const uint4*>((const T*)a.q + n * a.qs.item + t * a.qs.token + h * a.qs.head + at * 8), q);
-        Elem<T>::open(*reinterpret_cast<const uint4*>((const T*)a.dout + n * a.dos.item + t * a.dos.token + h * a.dos.head + at * 8), d);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        s = fmaf(q[e], kf[e], s);
-        dp = fmaf(d[e], vf[e], dp);
-      }
-      for (int w = gs >> 1; w > 0; w >>= 1) {
-        s += __shfl_xor_sync(0xffffffffu, s, w);
-        dp += __shfl_xor_sync(0xffffffffu, dp, w);
-      }
-      float p = 0.f, ds = 0.f;
-      if (there) {
-        const int64_t row = (n * a.Q + t) * a.H + h;
-        p = ex2(s * c2 - a.lse[row] * kLog2e);
-        ds = p * (dp - delta[row]);
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        dk[e] = fmaf(ds, q[e], dk[e]);
-        dv[e] = fmaf(p, d[e], dv[e]);
-      }
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    for (int w = gs; w < 32; w <<= 1) {
-      dk[e] += __shfl_xor_sync(0xffffffffu, dk[e], w);
-      dv[e] += __shfl_xor_sync(0xffffffffu, dv[e], w);
-    }
-    dk[e] *= a.scale;
-  }
-  if (lane < gs && col) {
-    *reinterpret_cast<uint4*>((T*)a.dk + g * a.dks.item + key * a.dks.token + j * a.dks.head + at * 8) = Elem<T>::pack(dk);
-    *reinterpret_cast<uint4*>((T*)a.dv + g * a.dvs.item + key * a.dvs.token + j * a.dvs.head + at * 8) = Elem<T>::pack(dv);
-  }
-}
-
-struct Plan {
-  size_t n, list, delta, total;
+// ===========================================================================
+// dq
+struct DqShape {
+  int kt, d16, stages, qbufs, tiles, groups, su;
+  uint32_t tmem;
 };
+constexpr int kTable = 256;
+
+template <int NWG>
+__host__ __device__ constexpr int dq_threads() {
+  return NWG * 128 + kLoadThreads + 32;
+}
+
+// stat: [item][key head][row of the key head] (lse log2 e, delta) for k_attn_dkv
+template <typename T, int NWG>
+__global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Keys keys, DqShape sh, float2* __restrict__ stat) {
+  constexpr int kBf16 = Elem<T>::kBf16;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[2], k_empty[2], s_full[NWG], p_full[NWG], o_full[NWG];
+  __shared__ uint32_t s_taddr;
+  __shared__ int2 s_work[kTable];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
+  const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2, cols = 2 * kt + d16;
+  unsigned char* sq = smem;                                 // per buffer and group: q, dout
+  unsigned char* sk = sq + sh.qbufs * NWG * 2 * qtile;      // per stage: k, v
+  unsigned char* so = sk + sh.stages * 2 * ktile;
+  if (tid == 0) {
+    for (int b = 0; b < 2; ++b) {
+      for (int g = 0; g < NWG; ++g) mbar_init(&q_full[b][g], kLoadThreads);
+      mbar_init(&q_empty[b], 1);
+      mbar_init(&k_full[b], kLoadThreads);
+      mbar_init(&k_empty[b], 1);
+    }
+    for (int g = 0; g < NWG; ++g) {
+      mbar_init(&s_full[g], 1);
+      mbar_init(&p_full[g], 4);
+      mbar_init(&o_full[g], 1);
+    }
+    fence_barrier_init();
+  }
+  if (D & 8) {  // the columns beyond D, once: no copy touches them
+    const int rows = sh.qbufs * NWG * 256 + 2 * sh.stages * kt;
+    for (int r = tid; r < rows; r += dq_threads<NWG>())
+      *reinterpret_cast<uint4*>(smem + (uint32_t)(r >> 3) * d16 * 16 + (d16 / 8 - 1) * 128 + (r & 7) * 16) =
+          make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  if (warp == 0) {
+    tmem_alloc(&s_taddr, sh.tmem);
+    tc_fence_before_sync();
+  }
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t taddr = s_taddr;
+  pdl_wait();
+  pdl_trigger();
+  const int works = items_of(a.count, a.N) * sh.groups * a.J;
+  struct Work {
+    int n, j, group, g, cnt;
+  };
+  auto look = [&](int w) {
+    const int g = source_of(a.src, a.src_stride, w / (a.J * sh.groups), a.G, a.status);
+    return make_int2(g, g < 0 ? 0 : keys.count(g));
+  };
+  for (int i = tid; i < kTable; i += dq_threads<NWG>()) {
+    const int64_t w = blockIdx.x + (int64_t)i * gridDim.x;
+    if (w < works) s_work[i] = look((int)w);
+  }
+  __syncthreads();
+  auto work = [&](int i, int w) {
+    Work k;
+    const int2 f = i < kTable ? s_work[i] : look(w);
+    k.g = f.x;
+    k.cnt = f.y;
+    k.j = w % a.J;
+    w /= a.J;
+    k.group = w % sh.groups;
+    k.n = w / sh.groups;
+    return k;
+  };
+  bool bad = false;
+
+  if (warp < 4 * NWG) {
+    // ================= a thread per row =================
+    const int g = warp >> 2;
+    const uint32_t tS = taddr + (uint32_t)g * cols + ((uint32_t)(warp & 3) << 21), tP = tS + kt, tO = tP + kt;
+    const float c2 = a.scale * kLog2e;
+    const int su = sh.su, sstride = su | 1;
+    const uint32_t usu = 65536u / su + 1;
+    unsigned char* stage = so + warp * 32 * sstride * 16;
+    uint32_t s_par = 0, o_par = 0;
+    int64_t pend = -1;  // this thread's row of dq still to be written (elements; negative: none)
+    bool pending = false;
+    auto finish = [&](int64_t row, bool empty) {
+      if (!empty) {
+        wait_or_bad(&o_full[g], o_par, bad, a.status);
+        o_par ^= 1;
+        __syncwarp();
+        tc_fence_after_sync();
+      }
+      const float scale = bad ? __int_as_float(0x7fffffff) : empty ? 0.f : a.scale;
+      for (int c0 = 0; c0 < D; c0 += su * 8) {
+        for (int c = c0; c < min(c0 + su * 8, D); c += 16) {
+          uint32_t r[16] = {};
+          if (!empty) {
+            tmem_ld(tO + c, r);
+            tmem_ld_wait();
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (h && c + 8 >= D) break;
+            float v[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(r[8 * h + q]) * scale;
+            *reinterpret_cast<uint4*>(stage + (lane * sstride + (c - c0) / 8 + h) * 16) = Elem<T>::pack(v);
+          }
+        }
+        __syncwarp();
+        const int units = min(su, (D - c0) / 8);
+        for (int q = 0; q < su; ++q) {
+          const uint32_t e = q * 32 + lane, r = (e * usu) >> 16, u = e - r * su;
+          const int64_t off = __shfl_sync(0xffffffffu, row, r);
+          if (off >= 0 && (int)u < units)
+            *reinterpret_cast<uint4*>((T*)a.dq + off + c0 + u * 8) =
+                *reinterpret_cast<const uint4*>(stage + (r * sstride + u) * 16);
+        }
+        __syncwarp();
+      }
+    };
+    for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
+      const Work k = work(i, w);
+      const int tile = k.group * NWG + g;
+      if (tile >= sh.tiles) continue;
+      const uint32_t m = (uint32_t)tile * 128 + (warp & 3) * 32 + lane;
+      const uint32_t t = R == 1 ? m : m / (uint32_t)R, h = k.j * R + (R == 1 ? 0 : m - t * R);
+      const bool there = t < (uint32_t)a.Q;
+      const int64_t row = there ? k.n * a.dqs.item + t * a.dqs.token + h * a.dqs.head : -1;
+      if (k.cnt <= 0) {
+        finish(row, true);
+        continue;
+      }
+      const float l2 = there ? a.lse[((int64_t)k.n * a.Q + t) * a.H + h] * kLog2e : 0.f;
+      float delta = 0.f;
+      const bool one = k.cnt <= kt;
+      for (int sweep = one ? 1 : 0; sweep < 2; ++sweep) {
+        for (int k0 = 0; k0 < k.cnt; k0 += kt) {
+          const int n = min(kt, k.cnt - k0), n16 = (n + 15) & ~15;
+          wait_or_bad(&s_full[g], s_par, bad, a.status);
+          s_par ^= 1;
+          __syncwarp();
+          tc_fence_after_sync();
+          if (sweep == 0 || one) {
+            float sum[4] = {};
+            for (int c = 0; c < n16; c += 16) {
+              uint32_t r[16], d[16];
+              tmem_ld(tS + c, r);
+              tmem_ld(tP + c, d);
+              tmem_ld_wait();
+#pragma unroll
+              for (int q = 0; q < 16; ++q) {
+                const float p = c + q < n ? ex2(fmaf(__uint_as_float(r[q]), c2, -l2)) : 0.f;
+                sum[q & 3] = fmaf(p, __uint_as_float(d[q]), sum[q & 3]);
+              }
+            }
+            delta += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          }
+          if (sweep == 1) {
+            for (int c = 0; c < n16; c += 16) {
+              uint32_t r[16], d[16], s[8];
+              tmem_ld(tS + c, r);
+              tmem_ld(tP + c, d);
+              tmem_ld_wait();
+#pragma unroll
+              for (int q = 0; q < 16; q += 2) {
+                float x = ex2(fmaf(__uint_as_float(r[q]), c2, -l2)) * (__uint_as_float(d[q]) - delta);
+                float y = ex2(fmaf(__uint_as_float(r[q + 1]), c2, -l2)) * (__uint_as_float(d[q + 1]) - delta);
+                x = c + q < n ? x : 0.f;
+                y = c + q + 1 < n ? y : 0.f;
+                s[q / 2] = Elem<T>::pack2(x, y);
+              }
+              tmem_st(tS + c / 2, s);
+            }
+            if (k0 == 0 && pending) finish(pend, false);
+            tmem_st_wait();
+          }
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&p_full[g]);
+        }
+      }
+      if (there) stat[((int64_t)k.n * a.J + k.j) * a.Q * R + m] = make_float2(l2, delta);
+      pend = row;
+      pending = true;
+    }
+    if (pending) finish(pend, false);
+  } else if (warp < 4 * NWG + kLoadWarps) {
+    // ================= loads =================
+    const int lt = tid - 4 * NWG * 32;
+    Jobs jobs;
+    uint32_t it = 0, qi = 0;
+    int hg = -1, hj = 0;  // the keys that stay
+    for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
+      const Work k = work(i, w);
+      if (k.cnt <= 0) continue;
+      const bool one = k.cnt <= kt, reuse = hg == k.g && hj == k.j;
+      hg = one ? k.g : -1;
+      hj = k.j;
+      const T* kp = (const T*)a.k + k.g * a.ks.item + k.j * a.ks.head;
+      const T* vp = (const T*)a.v + k.g * a.vs.item + k.j * a.vs.head;
+      const uint32_t qb = qi % sh.qbufs;
+      for (int sweep = one ? 1 : 0; sweep < 2; ++sweep) {
+        for (int k0 = 0; k0 < k.cnt; k0 += kt) {
+          if (!reuse) {
+            const uint32_t st = it % sh.stages;
+            if (it >= (uint32_t)sh.stages) jobs.wait(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
+            const int n = min(kt, k.cnt - k0);
+            copy_tile<T>(smem_u32(sk + st * 2 * ktile), (n + 15) & ~15, D, d16, kp, lt, [&](int r) {
+              return r < n ? kp + keys.at(k.g, k0 + r) * a.ks.token : (const T*)nullptr;
+            });
+            copy_tile<T>(smem_u32(sk + st * 2 * ktile + ktile), (n + 15) & ~15, D, d16, vp, lt, [&](int r) {
+              return r < n ? vp + keys.at(k.g, k0 + r) * a.vs.token : (const T*)nullptr;
+            });
+            jobs.push(&k_full[st]);
+            ++it;
+          }
+          if (k0 == 0 && sweep == (one ? 1 : 0)) {
+            if (qi >= (uint32_t)sh.qbufs) jobs.wait(&q_empty[qb], (qi / sh.qbufs - 1) & 1u, bad, a.status);
+            const T* qp = (const T*)a.q + k.n * a.qs.item + k.j * R * a.qs.head;
+            const T* dp = (const T*)a.dout + k.n * a.dos.item + k.j * R * a.dos.head;
+#pragma unroll 1
+            for (int g = 0; g < NWG; ++g) {
+              const int tile = k.group * NWG + g;
+              if (tile < sh.tiles) {
+                const uint32_t m0 = (uint32_t)tile * 128;
+                const uint32_t to = smem_u32(sq + (qb * NWG + g) * 2 * qtile);
+                auto rows = [&](const T* base, const Strides& s) {
+                  return [=](int r) {
+                    const uint32_t m = m0 + r, t = R == 1 ? m : m / (uint32_t)R;
+                    return t < (uint32_t)a.Q ? base + t * s.token + (R == 1 ? 0 : (m - t * R) * s.head) : (const T*)nullptr;
+                  };
+                };
+                copy_tile<T>(to, 128, D, d16, qp, lt, rows(qp, a.qs));
+                copy_tile<T>(to + qtile, 128, D, d16, dp, lt, rows(dp, a.dos));
+              }
+              jobs.push(&q_full[qb][g]);
+            }
+          }
+        }
+      }
+      ++qi;
+    }
+    jobs.flush();
+  } else if (lane == 0) {
+    // ================= MMAs =================
+    const uint32_t aq = smem_u32(sq), ak = smem_u32(sk), step = (uint32_t)d16 * 32;
+    uint32_t it = 0, qi = 0, p_par = 0;
+    int hg = -1, hj = 0;
+    bool pv[NWG], plast = false, pfirst = false, pmul = false, have = false;
+#pragma unroll
+    for (int g = 0; g < NWG; ++g) pv[g] = false;
+    uint32_t pst = 0;
+    int pn16 = 0;
+    auto second = [&](int g) {  // the step before is taken; dQ += dS K in the second sweep
+      wait_or_bad(&p_full[g], (p_par >> g) & 1u, bad, a.status);
+      p_par ^= 1u << g;
+      tc_fence_after_sync();
+      if (!pmul) return;
+      const uint32_t tS = taddr + (uint32_t)g * cols, idesc = tc_idesc_16(128, d16, kBf16, 0, 1);
+      for (int ks = 0; ks < pn16 / 16; ++ks)
+        tc_mma_f16_ta(tS + 2 * kt, tS + ks * 8, tile_desc_cols(ak + pst * 2 * ktile + ks * step, d16), idesc,
+                      !pfirst || ks > 0 ? 1u : 0u);
+      if (plast) tc_commit(&o_full[g]);
+    };
+    for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
+      const Work k = work(i, w);
+      if (k.cnt <= 0) continue;
+      const bool one = k.cnt <= kt, reuse = hg == k.g && hj == k.j;
+      hg = one ? k.g : -1;
+      hj = k.j;
+      const uint32_t qb = qi % sh.qbufs;
+      for (int sweep = one ? 1 : 0; sweep < 2; ++sweep) {
+        for (int k0 = 0; k0 < k.cnt; k0 += kt) {
+          const int n16 = (min(kt, k.cnt - k0) + 15) & ~15;
+          uint32_t st = pst;
+          if (!reuse) {
+            st = it % sh.stages;
+            // one stage: it has to be given back before it can be filled again
+            if (sh.stages == 1 && have) {
+#pragma unroll
+              for (int g = 0; g < NWG; ++g)
+                if (pv[g]) {
+                  second(g);
+                  pv[g] = false;
+                }
+              tc_commit(&k_empty[pst]);
+            }
+            wait_or_bad(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
+          }
+          const uint32_t idesc = tc_idesc_16(128, n16, kBf16, 0, 0);
+          const bool firsts = k0 == 0 && sweep == (one ? 1 : 0);
+#pragma unroll
+          for (int g = 0; g < NWG; ++g) {
+            if (pv[g]) second(g);
+            pv[g] = k.group * NWG + g < sh.tiles;
+            if (pv[g]) {
+              if (firsts) wait_or_bad(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+              tc_fence_after_sync();
+              const uint32_t tS = taddr + (uint32_t)g * cols, q = aq + (qb * NWG + g) * 2 * qtile, kk = ak + st * 2 * ktile;
+              for (int ks = 0; ks < d16 / 16; ++ks)
+                tc_mma_f16(tS, tile_desc_rows(q + ks * 256, d16), tile_desc_rows(kk + ks * 256, d16), idesc, ks > 0 ? 1u : 0u);
+              for (int ks = 0; ks < d16 / 16; ++ks)
+                tc_mma_f16(tS + kt, tile_desc_rows(q + qtile + ks * 256, d16), tile_desc_rows(kk + ktile + ks * 256, d16),
+                           idesc, ks > 0 ? 1u : 0u);
+              tc_commit(&s_full[g]);
+            }
+          }
+          if (have && !reuse && sh.stages > 1) tc_commit(&k_empty[pst]);
+          have = true;
+          if (!reuse) ++it;
+          pst = st;
+          pn16 = n16;
+          pmul = sweep == 1;
+          pfirst = k0 == 0;
+          plast = sweep == 1 && k0 + kt >= k.cnt;
+        }
+      }
+      tc_commit(&q_empty[qb]);
+      ++qi;
+    }
+#pragma unroll
+    for (int g = 0; g < NWG; ++g)
+      if (pv[g]) second(g);
+  }
+  __syncthreads();
+  __syncwarp();
+  if (warp == 0) tmem_dealloc(taddr, sh.tmem);
+}
+
+// ===========================================================================
+// dk and dv
+struct DkvShape {
+  int qt, d16, stages, kb, parts, halves;  // rows of a tile; key tiles; parts of the rows; parts of the columns
+  uint32_t tmem;
+};
+constexpr int kDkvStages = 4;
+constexpr int kDkvThreads = 2 * 128 + kLoadThreads + 32;
+constexpr int kKeyTile = 128;
+
+// part: [part][dv, dk][source][key head][key in the list][D]
+template <typename T>
+__global__ void __launch_bounds__(kDkvThreads, 1)
+    k_attn_dkv(AttnArgs a, Keys keys, DkvShape sh, const float2* __restrict__ stat, const int32_t* __restrict__ first,
+               const int32_t* __restrict__ order, float* __restrict__ part) {
+  constexpr int kBf16 = Elem<T>::kBf16;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ __align__(8) uint64_t q_full[kDkvStages], q_empty[kDkvStages], k_full, s_full[2], p_full[2], done;
+  __shared__ uint32_t s_taddr;
+  __shared__ __align__(16) float2 s_stat[kDkvStages][64];
+  __shared__ int64_t s_off[2][2][64];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int D = a.D, d16 = sh.d16, R = a.H / a.J, qt = sh.qt, rows_item = a.Q * R;
+  pdl_wait();
+  int b = blockIdx.x;
+  const int p = b % sh.parts;
+  b /= sh.parts;
+  const int half = b % sh.halves;
+  b /= sh.halves;
+  const int j = b % a.J;
+  b /= a.J;
+  const int kb = b % sh.kb, g = b / sh.kb;
+  const int k0 = kb * kKeyTile, kn = keys.count(g) - k0;
+  if (kn <= 0) return;
+  // the source's items
+  const int i0 = first ? first[2 * g] : g, i1 = first ? first[2 * g + 1] : g + (g < items_of(a.count, a.N));
+  const int64_t rows = (int64_t)(i1 - i0) * rows_item, all = (rows + qt - 1) / qt;
+  const int64_t t0 = all * p / sh.parts;
+  const int tiles = (int)(all * (p + 1) / sh.parts - t0);
+  // this CTA's columns of dv and dk
+  const int split16 = (d16 / 16 + sh.halves - 1) / sh.halves * 16;
+  const int c0 = half * split16, dn = min(split16, d16 - c0);
+  const uint32_t qtile = (uint32_t)qt * d16 * 2, ktile = (uint32_t)kKeyTile * d16 * 2;
+  unsigned char* sk = smem;
+  unsigned char* sv = sk + ktile;
+  unsigned char* sq = sv + ktile;  // per stage: q, dout
+  if (tid == 0) {
+    for (int s = 0; s < kDkvStages; ++s) {
+      mbar_init(&q_full[s], kLoadThreads);
+      mbar_init(&q_empty[s], 1);
+    }
+    mbar_init(&k_full, kLoadThreads);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(&s_full[s], 1);
+      mbar_init(&p_full[s], 4);
+    }
+    mbar_init(&done, 1);
+    fence_barrier_init();
+  }
+  if (D & 8) {
+    const int n = 2 * kKeyTile + sh.stages * 2 * qt;
+    for (int r = tid; r < n; r += kDkvThreads)
+      *reinterpret_cast<uint4*>(smem + (uint32_t)(r >> 3) * d16 * 16 + (d16 / 8 - 1) * 128 + (r & 7) * 16) =
+          make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
+  }
+  if (warp == 0) {
+    tmem_alloc(&s_taddr, sh.tmem);
+    tc_fence_before_sync();
+  }
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t taddr = s_taddr;
+  pdl_trigger();
+  bool bad = false;
+  const uint32_t acc = taddr + 4 * qt;  // dv, then dk
+  if (warp < 8) {
+    // ================= P^T and dS^T: a thread per key =================
+    const int s = warp >> 2;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21, tS = taddr + (uint32_t)s * 2 * qt + lanes, tP = tS + qt;
+    const float c2 = a.scale * kLog2e;
+    uint32_t par = 0;
+    for (int i = s; i < tiles; i += 2) {
+      wait_or_bad(&q_full[i % sh.stages], (i / sh.stages) & 1u, bad, a.status);  // lse and delta
+      wait_or_bad(&s_full[s], par, bad, a.status);
+      par ^= 1;
+      __syncwarp();
+      tc_fence_after_sync();
+      const float4* st = reinterpret_cast<const float4*>(s_stat[i % sh.stages]);
+      for (int c = 0; c < qt; c += 16) {
+        uint32_t r[16], d[16], pp[8], ds[8];
+        tmem_ld(tS + c, r);
+        tmem_ld(tP + c, d);
+        tmem_ld_wait();
+#pragma unroll
+        for (int q = 0; q < 16; q += 2) {
+          const float4 f = st[(c + q) / 2];  // lse, delta of two rows
+          const float x = ex2(fmaf(__uint_as_float(r[q]), c2, -f.x)), y = ex2(fmaf(__uint_as_float(r[q + 1]), c2, -f.z));
+          pp[q / 2] = Elem<T>::pack2(x, y);
+          ds[q / 2] = Elem<T>::pack2(x * (__uint_as_float(d[q]) - f.y), y * (__uint_as_float(d[q + 1]) - f.w));
+        }
+        tmem_st(tS + c / 2, pp);
+        tmem_st(tP + c / 2, ds);
+      }
+      tmem_st_wait();
+      tc_fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_full[s]);
+    }
+    // one group writes dv, the other dk
+    if (tiles > 0) wait_or_bad(&done, 0, bad, a.status);
+    __syncwarp();
+    tc_fence_after_sync();
+    const int row = (warp & 3) * 32 + lane;
+    const int64_t states = (int64_t)a.G * a.J * a.K;
+    float* o = part + (((int64_t)(p * 2 + s)) * states + ((int64_t)g * a.J + j) * a.K + k0 + row) * D;
+    const float scale = bad ? __int_as_float(0x7fffffff) : s ? a.scale : 1.f;
+    for (int c = 0; c < dn; c += 16) {
+      uint32_t r[16] = {};
+      if (tiles > 0) {
+        tmem_ld(acc + s * dn + lanes + c, r);
+        tmem_ld_wait();
+      }
+      if (row < kn) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          if (c0 + c + 4 * q < D)
+            *reinterpret_cast<float4*>(o + c0 + c + 4 * q) =
+                make_float4(__uint_as_float(r[4 * q]) * scale, __uint_as_float(r[4 * q + 1]) * scale,
+                            __uint_as_float(r[4 * q + 2]) * scale, __uint_as_float(r[4 * q + 3]) * scale);
+      }
+    }
+  } else if (warp < 8 + kLoadWarps) {
+    // ================= loads =================
+    const int lt = tid - 256;
+    Jobs jobs;
+    if (tiles > 0) {
+      const T* kp = (const T*)a.k + g * a.ks.item + j * a.ks.head;
+      const T* vp = (const T*)a.v + g * a.vs.item + j * a.vs.head;
+      copy_tile<T>(smem_u32(sk), kKeyTile, D, d16, kp, lt, [&](int r) {
+        return r < kn ? kp + keys.at(g, k0 + r) * a.ks.token : (const T*)nullptr;
+      });
+      copy_tile<T>(smem_u32(sv), kKeyTile, D, d16, vp, lt, [&](int r) {
+        return r < kn ? vp + keys.at(g, k0 + r) * a.vs.token : (const T*)nullptr;
+      });
+      jobs.push(&k_full);
+    }
+    for (int i = 0; i < tiles; ++i) {
+      const uint32_t st = i % sh.stages;
+      if (i >= sh.stages) jobs.wait(&q_empty[st], (i / sh.stages - 1) & 1u, bad, a.status);
+      // where the rows lie
+      if (lt < qt) {
+        const int64_t m = (t0 + i) * qt + lt;
+        int64_t oq = -1, od = -1;
+        const float2* f = stat;
+        if (m < rows) {
+          const int it = (int)(m / rows_item), r = (int)(m - (int64_t)it * rows_item), t = r / R, h = j * R + r % R;
+          const int64_t n = order ? order[i0 + it] : i0 + it;
+          oq = n * a.qs.item + t * a.qs.token + h * a.qs.head;
+          od = n * a.dos.item + t * a.dos.token + h * a.dos.head;
+          f = stat + (n * a.J + j) * rows_item + r;
+        }
+        s_off[i & 1][0][lt] = oq;
+        s_off[i & 1][1][lt] = od;
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(&s_stat[st][lt])), "l"(f),
+                     "r"(oq >= 0 ? 8 : 0)
+                     : "memory");
+      }
+      asm volatile("bar.sync 1, %0;" ::"n"(kLoadThreads) : "memory");
+      const int64_t* off = s_off[i & 1][0];
+      copy_tile<T>(smem_u32(sq + st * 2 * qtile), qt, D, d16, (const T*)a.q, lt, [&](int r) {
+        return off[r] >= 0 ? (const T*)a.q + off[r] : (const T*)nullptr;
+      });
+      copy_tile<T>(smem_u32(sq + st * 2 * qtile + qtile), qt, D, d16, (const T*)a.dout, lt, [&](int r) {
+        return off[64 + r] >= 0 ? (const T*)a.dout + off[64 + r] : (const T*)nullptr;
+      });
+      jobs.push(&q_full[st]);
+    }
+    jobs.flush();
+  } else if (lane == 0 && tiles > 0) {
+    // ================= MMAs =================
+    const uint32_t ak = smem_u32(sk), av = smem_u32(sv), aq = smem_u32(sq), step = (uint32_t)d16 * 32;
+    const uint32_t idesc = tc_idesc_16(128, qt, kBf16, 0, 0), idesc2 = tc_idesc_16(128, dn, kBf16, 0, 1);
+    uint32_t p_par = 0;
+    wait_or_bad(&k_full, 0, bad, a.status);
+    auto scores = [&](int i) {
+      const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt, q = aq + st * 2 * qtile;
+      wait_or_bad(&q_full[st], (i / sh.stages) & 1u, bad, a.status);
+      tc_fence_after_sync();
+      for (int ks = 0; ks < d16 / 16; ++ks)
+        tc_mma_f16(tS, tile_desc_rows(ak + ks * 256, d16), tile_desc_rows(q + ks * 256, d16), idesc, ks > 0 ? 1u : 0u);
+      for (int ks = 0; ks < d16 / 16; ++ks)
+        tc_mma_f16(tS + qt, tile_desc_rows(av + ks * 256, d16), tile_desc_rows(q + qtile + ks * 256, d16), idesc,
+                   ks > 0 ? 1u : 0u);
+      tc_commit(&s_full[s]);
+    };
+    scores(0);
+    if (tiles > 1) scores(1);
+    for (int i = 0; i < tiles; ++i) {
+      const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt, q = aq + st * 2 * qtile;
+      wait_or_bad(&p_full[s], (p_par >> s) & 1u, bad, a.status);
+      p_par ^= 1u << s;
+      tc_fence_after_sync();
+      for (int ks = 0; ks < qt / 16; ++ks)
+        tc_mma_f16_ta(acc, tS + ks * 8, tile_desc_cols(q + qtile + ks * step + c0 * 16, d16), idesc2, i > 0 || ks > 0 ? 1u : 0u);
+      for (int ks = 0; ks < qt / 16; ++ks)
+        tc_mma_f16_ta(acc + dn, tS + qt + ks * 8, tile_desc_cols(q + ks * step + c0 * 16, d16), idesc2,
+                      i > 0 || ks > 0 ? 1u : 0u);
+      tc_commit(&q_empty[st]);
+      if (i + 2 < tiles) scores(i + 2);
+    }
+    tc_commit(&done);
+  }
+  __syncthreads();
+  __syncwarp();
+  if (warp == 0) tmem_dealloc(taddr, sh.tmem);
+}
+
+// The parts of dv and dk in order; eight values of a key to a thread. Keys that
+// do not count get zeros. pos: a key's place in its source's list (mask only).
+template <typename T>
+__global__ void __launch_bounds__(256) k_attn_sum(AttnArgs a, Keys keys, const int32_t* __restrict__ pos, int parts,
+                                                 const float* __restrict__ part) {
+  pdl_wait();
+  pdl_trigger();
+  const int pieces = a.D / 8;
+  const int64_t states = (int64_t)a.G * a.J * a.K, all = 2 * states * pieces;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < all; e += (int64_t)gridDim.x * 256) {
+    const int c = (int)(e % pieces) * 8;
+    int64_t x = e / pieces;
+    const int j = (int)(x % a.J);
+    x /= a.J;
+    const int key = (int)(x % a.K);
+    x /= a.K;
+    const int g = (int)(x % a.G), which = (int)(x / a.G);
+    const int at = pos ? pos[(int64_t)g * a.K + key] : key < keys.count(g) ? key : -1;
+    float v[8] = {};
+    if (at >= 0) {
+      const float* s = part + (which * states + ((int64_t)g * a.J + j) * a.K + at) * a.D + c;
+#pragma unroll 4
+      for (int p = 0; p < parts; ++p) {
+        const float4* q = reinterpret_cast<const float4*>(s + (int64_t)p * 2 * states * a.D);
+        const float4 u = __ldcg(q), w = __ldcg(q + 1);
+        v[0] += u.x;
+        v[1] += u.y;
+        v[2] += u.z;
+        v[3] += u.w;
+        v[4] += w.x;
+        v[5] += w.y;
+        v[6] += w.z;
+        v[7] += w.w;
+      }
+    }
+    const Strides& s = which ? a.dks : a.dvs;
+    *reinterpret_cast<uint4*>((T*)(which ? a.dk : a.dv) + g * s.item + key * s.token + j * s.head + c) = Elem<T>::pack(v);
+  }
+}
+
+// ---- shapes and workspace -------------------------------------------------------
+struct Plan {
+  int nwg, grid;
+  DqShape dq;
+  size_t dq_smem;
+  DkvShape kv;
+  size_t kv_smem;
+  size_t n, list, pos, first, order, stat, part, total;
+};
+
 Plan plan(const AttnArgs& a) {
   Plan p{};
+  const int d16 = (a.D + 15) & ~15, k16 = a.K > 0 ? (a.K + 15) & ~15 : 16;
+  const int64_t rows = (int64_t)a.Q * (a.H / a.J);
+  // dq: two groups of softmax warps where S, dP and dQ of both fit TMEM with key tiles of 48 or more
+  DqShape& s = p.dq;
+  s.d16 = d16;
+  s.tiles = (int)((rows + 127) / 128);
+  p.nwg = 2;
+  s.kt = ((256 - d16) / 2) & ~15;
+  if (s.kt < 48 || s.tiles < 2) {
+    p.nwg = 1;
+    s.kt = ((512 - d16) / 2) & ~15;
+  }
+  if (s.kt > 128) s.kt = 128;
+  if (s.kt > k16) s.kt = k16;
+  s.su = a.D / 8 < 8 ? a.D / 8 : a.D > 64 ? 4 : 8;
+  s.qbufs = 2;
+  s.stages = 2;
+  const auto dq_smem = [&] {
+    return ((size_t)s.qbufs * p.nwg * 256 + 2 * (size_t)s.stages * s.kt) * d16 * 2 + (size_t)p.nwg * 128 * (s.su | 1) * 16;
+  };
+  while (dq_smem() > kSmemMost) {
+    if (s.qbufs == 2) s.qbufs = 1;
+    else if (s.kt > 48) s.kt -= 16;
+    else if (p.nwg > 1) --p.nwg;
+    else s.stages = 1;
+  }
+  p.dq_smem = dq_smem();
+  s.groups = (s.tiles + p.nwg - 1) / p.nwg;
+  s.tmem = 32;
+  while (s.tmem < (uint32_t)(p.nwg * (2 * s.kt + d16))) s.tmem <<= 1;
+  const int64_t works = (int64_t)a.N * s.groups * a.J;
+  p.grid = (int)(works < kSms ? works : kSms);
+  if (a.K <= s.kt && a.J < kSms && works > kSms) p.grid -= kSms % a.J;  // a CTA keeps its head
+  // dk, dv
+  DkvShape& v = p.kv;
+  v.d16 = d16;
+  v.halves = d16 > 192 ? 2 : 1;
+  const int dn = (d16 / 16 + v.halves - 1) / v.halves * 16;
+  v.qt = (512 - 2 * dn) / 4 & ~15;
+  if (v.qt > 64) v.qt = 64;
+  v.stages = kDkvStages;
+  const auto kv_smem = [&] { return (2 * (size_t)kKeyTile + (size_t)v.stages * 2 * v.qt) * d16 * 2; };
+  while (kv_smem() > kSmemMost - 8192) {
+    if (v.stages > 2) --v.stages;
+    else v.qt -= 16;
+  }
+  p.kv_smem = kv_smem();
+  v.tmem = 32;
+  while (v.tmem < (uint32_t)(4 * v.qt + 2 * dn)) v.tmem <<= 1;
+  v.kb = (a.K + kKeyTile - 1) / kKeyTile;
+  // about three CTAs per SM in all: key tiles that do not count end at once
+  const int64_t units = (int64_t)a.G * a.J * v.kb * v.halves;
+  const int64_t tiles = ((int64_t)a.N * rows + v.qt - 1) / v.qt;
+  int64_t parts = units > 0 ? (3 * kSms + units - 1) / units : 1;
+  if (v.kb == 1 && units > 0) parts = kSms / units;  // every key tile counts: one CTA per SM
+  if (parts > tiles / 4) parts = tiles / 4;
+  v.parts = parts < 1 ? 1 : (int)parts;
   size_t o = 0;
   auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, kAlign); return at; };
   if (a.mask) {
     p.n = take((size_t)a.G * 4);
     p.list = take((size_t)a.G * a.K * 4);
+    p.pos = take((size_t)a.G * a.K * 4);
   }
-  p.delta = take((size_t)a.N * a.Q * a.H * 4);
+  p.first = take((size_t)a.G * 8);
+  p.order = take((size_t)a.N * 4);
+  p.stat = take((size_t)a.N * a.J * rows * 8);
+  p.part = take((size_t)v.parts * 2 * a.G * a.J * a.K * a.D * 4);
   p.total = o;
   return p;
+}
+
+template <typename T, int NWG>
+cudaError_t go_dq(const AttnArgs& a, const Keys& keys, const Plan& p, float2* stat, cudaStream_t st) {
+  static SmemGranted granted;
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_dq<T, NWG>), p.dq_smem, granted);
+  if (e != cudaSuccess) return e;
+  return launch_ex(k_attn_dq<T, NWG>, dim3(p.grid), dim3(dq_threads<NWG>()), p.dq_smem, st, 0, a, keys, p.dq, stat);
 }
 
 template <typename T>
@@ -154,24 +758,42 @@ cudaError_t run(const AttnArgs& a, cudaStream_t st) {
   const Plan p = plan(a);
   Keys keys{a.K, a.len, nullptr, nullptr};
   cudaError_t e = cudaSuccess;
-  if (a.mask) {
+  int32_t* pos = nullptr;
+  if (a.mask && a.G > 0) {
     int32_t* n = reinterpret_cast<int32_t*>(a.ws + p.n);
     int32_t* list = reinterpret_cast<int32_t*>(a.ws + p.list);
-    e = launch_attn_keys(a, n, list, st);
+    pos = reinterpret_cast<int32_t*>(a.ws + p.pos);
+    e = launch_attn_keys(a, n, list, pos, st);
     if (e != cudaSuccess) return e;
     keys.n = n;
     keys.list = list;
   }
-  int gs = 1;
-  while (gs * 8 < a.D) gs <<= 1;
-  float* delta = reinterpret_cast<float*>(a.ws + p.delta);
-  const int64_t rows = (int64_t)a.N * a.Q * a.H, units = (int64_t)a.G * a.J * a.K;
-  if (rows > 0) {
-    e = launch_ex(k_attn_dq<T>, dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, 0, a, keys, gs, delta);
+  int32_t* first = nullptr;
+  int32_t* order = nullptr;
+  if (a.src && a.G > 0) {
+    first = reinterpret_cast<int32_t*>(a.ws + p.first);
+    order = reinterpret_cast<int32_t*>(a.ws + p.order);
+    e = launch_ex(k_attn_order, dim3(a.G), dim3(kOrderThreads), 0, st, 0, a.src, a.src_stride, a.count, a.N, first, order);
     if (e != cudaSuccess) return e;
   }
-  if (units == 0) return cudaSuccess;
-  return launch_ex(k_attn_dkv<T>, dim3((unsigned)((units + 7) / 8)), dim3(256), 0, st, 0, a, keys, gs, (const float*)delta);
+  float2* stat = reinterpret_cast<float2*>(a.ws + p.stat);
+  float* part = reinterpret_cast<float*>(a.ws + p.part);
+  if (p.grid > 0) {
+    e = p.nwg == 1 ? go_dq<T, 1>(a, keys, p, stat, st) : go_dq<T, 2>(a, keys, p, stat, st);
+    if (e != cudaSuccess) return e;
+  }
+  const int64_t pieces = (int64_t)a.G * a.J * a.K * (a.D / 8) * 2;
+  if (pieces == 0) return cudaSuccess;
+  static SmemGranted granted;
+  e = allow_smem(reinterpret_cast<const void*>(k_attn_dkv<T>), p.kv_smem, granted);
+  if (e != cudaSuccess) return e;
+  const int64_t grid = (int64_t)a.G * a.J * p.kv.kb * p.kv.halves * p.kv.parts;
+  e = launch_ex(k_attn_dkv<T>, dim3((unsigned)grid), dim3(kDkvThreads), p.kv_smem, st, 0, a, keys, p.kv, (const float2*)stat,
+                (const int32_t*)first, (const int32_t*)order, part);
+  if (e != cudaSuccess) return e;
+  const int64_t ctas = (pieces + 255) / 256;
+  return launch_ex(k_attn_sum<T>, dim3((unsigned)(ctas < 1216 ? ctas : 1216)), dim3(256), 0, st, 0, a, keys,
+                   (const int32_t*)pos, p.kv.parts, (const float*)part);
 }
 
 }  // namespace

@@ -134,7 +134,7 @@ __device__ __forceinline__ void copy_tile(uint32_t dst, int rows, int d, int d16
 }
 
 // The list above (k_attn.cu).
-cudaError_t launch_attn_keys(const AttnArgs& a, int32_t* n, int32_t* list, cudaStream_t st);
+cudaError_t launch_attn_keys(const AttnArgs& a, int32_t* n, int32_t* list, int32_t* pos, cudaStream_t st);
 // The forward pass on the tensor cores (k_attn_tc.cu); parts of the keys, 1:
 // none, else po [row][part][D] and pl [row][part] are written for the join.
 int attn_tc_splits(const AttnArgs& a);
