@@ -48,21 +48,9 @@ class PaSrdsStats(C.Structure):
         return {k: getattr(self, k) for k, _ in self._fields_ if k != "reserved"}
 
 
-class PaAttention(C.Structure):
-    """pa_attention_t; the fields behind ``lse`` are the backward pass's."""
-    _fields_ = [("dtype", C.c_int32), ("items", C.c_int32), ("tokens", C.c_int32), ("sources", C.c_int32),
-                ("keys", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
-                ("scale", C.c_double), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
-                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
-                ("source", C.c_void_p), ("source_stride", C.c_int64), ("lengths", C.c_void_p), ("mask", C.c_void_p),
-                ("mask_stride", C.c_int64), ("n_items_dev", C.c_void_p), ("out", C.c_void_p),
-                ("out_stride", C.c_int64 * 3), ("lse", C.c_void_p), ("dout", C.c_void_p), ("dq", C.c_void_p),
-                ("dk", C.c_void_p), ("dv", C.c_void_p), ("dout_stride", C.c_int64 * 3), ("dq_stride", C.c_int64 * 3),
-                ("dk_stride", C.c_int64 * 3), ("dv_stride", C.c_int64 * 3)]
-
-
 PA_F32, PA_F16, PA_BF16 = 0, 1, 2
 
+_NO_SIZE = C.c_size_t(-1).value
 _lib = None
 VP = C.c_void_p
 PVP = C.POINTER(C.c_void_p)
@@ -133,9 +121,9 @@ _PROTOS = {
     "pa_layer_norm_backward_workspace_bytes": (C.c_size_t, [C.c_int64, C.c_int]),
     "pa_layer_norm_backward": (C.c_int, [C.c_int, C.c_int64, C.c_int, VP, C.c_int64, VP, C.c_int64, VP, VP, VP, VP,
                                          C.c_int64, VP, VP, VP, C.c_int64, VP, C.c_size_t, VP]),
-    "pa_attention_workspace_bytes": (C.c_size_t, [C.POINTER(PaAttention), C.c_int]),
-    "pa_attention": (C.c_int, [C.POINTER(PaAttention), VP, C.c_size_t, VP]),
-    "pa_attention_backward": (C.c_int, [C.POINTER(PaAttention), VP, C.c_size_t, VP]),
+    "pa_attention_workspace_bytes": (C.c_size_t, [VP, C.c_int]),
+    "pa_attention": (C.c_int, [VP, VP, C.c_size_t, VP]),
+    "pa_attention_backward": (C.c_int, [VP, VP, C.c_size_t, VP]),
     "pa_attention_check": (C.c_int, [VP]),
     "pa_status_string": (C.c_char_p, [C.c_int]),
     "pa_last_error": (C.c_char_p, []),
@@ -507,9 +495,11 @@ def pa_layer_norm_backward(dtype, rows, cols, dy_ptr, dy_stride, x_ptr, x_stride
         dweight_ptr, dbias_ptr, n_items_dev_ptr, rows_per_item, workspace_ptr, workspace_bytes, stream_ptr))
 
 
+# a: pa_attention_t as bytes, or its address
+
 def pa_attention_workspace_bytes(a, backward):
     n = int(lib().pa_attention_workspace_bytes(a, int(backward)))
-    if n == C.c_size_t(-1).value:
+    if n == _NO_SIZE:
         raise PaError("pa_attention_workspace_bytes", PA_ERR_ARG, last_error())
     return n
 

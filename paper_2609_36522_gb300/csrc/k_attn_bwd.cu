@@ -22,7 +22,7 @@ namespace pa {
 namespace {
 
 constexpr int kSms = 152;
-constexpr size_t kSmemMost = 224 << 10;
+constexpr size_t kSmemMost = 222 << 10;
 
 // Sources' items in order, by source: a CTA per source.
 constexpr int kOrderThreads = 256;
@@ -72,6 +72,7 @@ struct DqShape {
 };
 constexpr int kTable = 256;
 
+constexpr int kLoadThreads = 7 * 32;  // with the warp that issues the MMAs a multiple of four warps
 template <int NWG>
 __host__ __device__ constexpr int dq_threads() {
   return NWG * 128 + kLoadThreads + 32;
@@ -85,6 +86,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
   __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[2], k_empty[2], s_full[NWG], p_full[NWG], o_full[NWG];
   __shared__ uint32_t s_taddr;
   __shared__ int2 s_work[kTable];
+  __shared__ int64_t s_rows[2][128];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
   const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2, cols = 2 * kt + d16;
@@ -260,10 +262,10 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
       pending = true;
     }
     if (pending) finish(pend, false);
-  } else if (warp < 4 * NWG + kLoadWarps) {
+  } else if (warp < 4 * NWG + kLoadThreads / 32) {
     // ================= loads =================
     const int lt = tid - 4 * NWG * 32;
-    Jobs jobs;
+    RowTables<kLoadThreads> tab{s_rows, 0};
     uint32_t it = 0, qi = 0;
     int hg = -1, hj = 0;  // the keys that stay
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
@@ -279,19 +281,16 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
         for (int k0 = 0; k0 < k.cnt; k0 += kt) {
           if (!reuse) {
             const uint32_t st = it % sh.stages;
-            if (it >= (uint32_t)sh.stages) jobs.wait(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
+            if (it >= (uint32_t)sh.stages) wait_or_bad(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
             const int n = min(kt, k.cnt - k0);
-            copy_tile<T>(smem_u32(sk + st * 2 * ktile), (n + 15) & ~15, D, d16, kp, lt, [&](int r) {
-              return r < n ? kp + keys.at(k.g, k0 + r) * a.ks.token : (const T*)nullptr;
-            });
-            copy_tile<T>(smem_u32(sk + st * 2 * ktile + ktile), (n + 15) & ~15, D, d16, vp, lt, [&](int r) {
-              return r < n ? vp + keys.at(k.g, k0 + r) * a.vs.token : (const T*)nullptr;
-            });
-            jobs.push(&k_full[st]);
+            const uint32_t to = smem_u32(sk + st * 2 * ktile);
+            copy_keys<kLoadThreads, T>(tab, to, kp, a.ks.token, keys, k.g, k0, n, (n + 15) & ~15, D, d16, lt);
+            copy_keys<kLoadThreads, T>(tab, to + ktile, vp, a.vs.token, keys, k.g, k0, n, (n + 15) & ~15, D, d16, lt);
+            copies_arrive(&k_full[st]);
             ++it;
           }
           if (k0 == 0 && sweep == (one ? 1 : 0)) {
-            if (qi >= (uint32_t)sh.qbufs) jobs.wait(&q_empty[qb], (qi / sh.qbufs - 1) & 1u, bad, a.status);
+            if (qi >= (uint32_t)sh.qbufs) wait_or_bad(&q_empty[qb], (qi / sh.qbufs - 1) & 1u, bad, a.status);
             const T* qp = (const T*)a.q + k.n * a.qs.item + k.j * R * a.qs.head;
             const T* dp = (const T*)a.dout + k.n * a.dos.item + k.j * R * a.dos.head;
 #pragma unroll 1
@@ -300,23 +299,17 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
               if (tile < sh.tiles) {
                 const uint32_t m0 = (uint32_t)tile * 128;
                 const uint32_t to = smem_u32(sq + (qb * NWG + g) * 2 * qtile);
-                auto rows = [&](const T* base, const Strides& s) {
-                  return [=](int r) {
-                    const uint32_t m = m0 + r, t = R == 1 ? m : m / (uint32_t)R;
-                    return t < (uint32_t)a.Q ? base + t * s.token + (R == 1 ? 0 : (m - t * R) * s.head) : (const T*)nullptr;
-                  };
-                };
-                copy_tile<T>(to, 128, D, d16, qp, lt, rows(qp, a.qs));
-                copy_tile<T>(to + qtile, 128, D, d16, dp, lt, rows(dp, a.dos));
+                copy_queries<kLoadThreads, T>(tab, to, qp, a.qs, m0, R, a.Q, D, d16, lt);
+                copy_queries<kLoadThreads, T>(tab, to + qtile, dp, a.dos, m0, R, a.Q, D, d16, lt);
               }
-              jobs.push(&q_full[qb][g]);
+              copies_arrive(&q_full[qb][g]);
             }
           }
         }
       }
       ++qi;
     }
-    jobs.flush();
+    copies_drain();
   } else if (lane == 0) {
     // ================= MMAs =================
     const uint32_t aq = smem_u32(sq), ak = smem_u32(sk), step = (uint32_t)d16 * 32;
@@ -361,7 +354,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
                 }
               tc_commit(&k_empty[pst]);
             }
-            wait_or_bad(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
+            landed(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
           }
           const uint32_t idesc = tc_idesc_16(128, n16, kBf16, 0, 0);
           const bool firsts = k0 == 0 && sweep == (one ? 1 : 0);
@@ -370,7 +363,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
             if (pv[g]) second(g);
             pv[g] = k.group * NWG + g < sh.tiles;
             if (pv[g]) {
-              if (firsts) wait_or_bad(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+              if (firsts) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
               tc_fence_after_sync();
               const uint32_t tS = taddr + (uint32_t)g * cols, q = aq + (qb * NWG + g) * 2 * qtile, kk = ak + st * 2 * ktile;
               for (int ks = 0; ks < d16 / 16; ++ks)
@@ -423,7 +416,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
   __shared__ __align__(8) uint64_t q_full[kDkvStages], q_empty[kDkvStages], k_full, s_full[2], p_full[2], done;
   __shared__ uint32_t s_taddr;
   __shared__ __align__(16) float2 s_stat[kDkvStages][64];
-  __shared__ int64_t s_off[2][2][64];
+  __shared__ int64_t s_off[2][2][64], s_rows[2][128];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, qt = sh.qt, rows_item = a.Q * R;
   pdl_wait();
@@ -535,24 +528,21 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
                             __uint_as_float(r[4 * q + 2]) * scale, __uint_as_float(r[4 * q + 3]) * scale);
       }
     }
-  } else if (warp < 8 + kLoadWarps) {
+  } else if (warp < 8 + kLoadThreads / 32) {
     // ================= loads =================
     const int lt = tid - 256;
-    Jobs jobs;
+    RowTables<kLoadThreads> tab{s_rows, 0};
     if (tiles > 0) {
       const T* kp = (const T*)a.k + g * a.ks.item + j * a.ks.head;
       const T* vp = (const T*)a.v + g * a.vs.item + j * a.vs.head;
-      copy_tile<T>(smem_u32(sk), kKeyTile, D, d16, kp, lt, [&](int r) {
-        return r < kn ? kp + keys.at(g, k0 + r) * a.ks.token : (const T*)nullptr;
-      });
-      copy_tile<T>(smem_u32(sv), kKeyTile, D, d16, vp, lt, [&](int r) {
-        return r < kn ? vp + keys.at(g, k0 + r) * a.vs.token : (const T*)nullptr;
-      });
-      jobs.push(&k_full);
+      const int n = min(kn, kKeyTile);
+      copy_keys<kLoadThreads, T>(tab, smem_u32(sk), kp, a.ks.token, keys, g, k0, n, kKeyTile, D, d16, lt);
+      copy_keys<kLoadThreads, T>(tab, smem_u32(sv), vp, a.vs.token, keys, g, k0, n, kKeyTile, D, d16, lt);
+      copies_arrive(&k_full);
     }
     for (int i = 0; i < tiles; ++i) {
       const uint32_t st = i % sh.stages;
-      if (i >= sh.stages) jobs.wait(&q_empty[st], (i / sh.stages - 1) & 1u, bad, a.status);
+      if (i >= sh.stages) wait_or_bad(&q_empty[st], (i / sh.stages - 1) & 1u, bad, a.status);
       // where the rows lie
       if (lt < qt) {
         const int64_t m = (t0 + i) * qt + lt;
@@ -572,25 +562,21 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
                      : "memory");
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kLoadThreads) : "memory");
-      const int64_t* off = s_off[i & 1][0];
-      copy_tile<T>(smem_u32(sq + st * 2 * qtile), qt, D, d16, (const T*)a.q, lt, [&](int r) {
-        return off[r] >= 0 ? (const T*)a.q + off[r] : (const T*)nullptr;
-      });
-      copy_tile<T>(smem_u32(sq + st * 2 * qtile + qtile), qt, D, d16, (const T*)a.dout, lt, [&](int r) {
-        return off[64 + r] >= 0 ? (const T*)a.dout + off[64 + r] : (const T*)nullptr;
-      });
-      jobs.push(&q_full[st]);
+      const uint32_t to = smem_u32(sq + st * 2 * qtile);
+      copy_rows_at<kLoadThreads, T>(to, qt, D, d16, (const T*)a.q, s_off[i & 1][0], lt);
+      copy_rows_at<kLoadThreads, T>(to + qtile, qt, D, d16, (const T*)a.dout, s_off[i & 1][1], lt);
+      copies_arrive(&q_full[st]);
     }
-    jobs.flush();
+    copies_drain();
   } else if (lane == 0 && tiles > 0) {
     // ================= MMAs =================
     const uint32_t ak = smem_u32(sk), av = smem_u32(sv), aq = smem_u32(sq), step = (uint32_t)d16 * 32;
     const uint32_t idesc = tc_idesc_16(128, qt, kBf16, 0, 0), idesc2 = tc_idesc_16(128, dn, kBf16, 0, 1);
     uint32_t p_par = 0;
-    wait_or_bad(&k_full, 0, bad, a.status);
+    landed(&k_full, 0, bad, a.status);
     auto scores = [&](int i) {
       const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt, q = aq + st * 2 * qtile;
-      wait_or_bad(&q_full[st], (i / sh.stages) & 1u, bad, a.status);
+      landed(&q_full[st], (i / sh.stages) & 1u, bad, a.status);
       tc_fence_after_sync();
       for (int ks = 0; ks < d16 / 16; ++ks)
         tc_mma_f16(tS, tile_desc_rows(ak + ks * 256, d16), tile_desc_rows(q + ks * 256, d16), idesc, ks > 0 ? 1u : 0u);
@@ -715,7 +701,7 @@ Plan plan(const AttnArgs& a) {
   if (v.qt > 64) v.qt = 64;
   v.stages = kDkvStages;
   const auto kv_smem = [&] { return (2 * (size_t)kKeyTile + (size_t)v.stages * 2 * v.qt) * d16 * 2; };
-  while (kv_smem() > kSmemMost - 8192) {
+  while (kv_smem() > kSmemMost - 4096) {
     if (v.stages > 2) --v.stages;
     else v.qt -= 16;
   }

@@ -13,7 +13,7 @@
 // work item is read only after the next one's P is written, so no group waits for
 // its MMAs there.
 //
-// Three loader warps copy Q, K and V with 16-byte asynchronous copies, ahead of use;
+// The loader warps copy Q, K and V with 16-byte asynchronous copies, ahead of use;
 // keys are picked from the list of those that count. Where all keys are one tile and the next
 // work item has the same ones (rows of one trajectory), K and V stay in shared
 // memory: CTAs take work items in turn, heads innermost, so that a CTA keeps its
@@ -36,20 +36,28 @@ struct TcShape {
 
 __host__ __device__ inline int stage_units(int D) { return D / 8 < 8 ? D / 8 : 8; }  // 16-byte units of a staged row
 
+// Loader warps: with the warp that issues the MMAs a multiple of four (registers
+// are given out by four warps). Two groups go over many key tiles, whose copies
+// are most of the loaders' work.
+template <int NWG>
+__host__ __device__ constexpr int tc_load() {
+  return (NWG <= 2 ? 7 : 3) * 32;
+}
 template <int NWG>
 __host__ __device__ constexpr int tc_threads() {
-  return NWG * 128 + kLoadThreads + 32;
+  return NWG * 128 + tc_load<NWG>() + 32;
 }
 
 template <typename T, int NWG>
 __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
     k_attn_tc(AttnArgs a, Keys keys, TcShape sh, float* __restrict__ po, float* __restrict__ pl) {
-  constexpr int kBf16 = Elem<T>::kBf16;
+  constexpr int kBf16 = Elem<T>::kBf16, LT = tc_load<NWG>();
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[NWG],
       p_full[NWG], o_full[NWG];
   __shared__ uint32_t s_taddr;
   __shared__ int2 s_work[kTable];
+  __shared__ int64_t s_rows[2][128];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
   const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2;
@@ -59,11 +67,11 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   unsigned char* so = sv + sh.stages * ktile;
   if (tid == 0) {
     for (int b = 0; b < 2; ++b) {
-      for (int g = 0; g < NWG; ++g) mbar_init(&q_full[b][g], kLoadThreads);
+      for (int g = 0; g < NWG; ++g) mbar_init(&q_full[b][g], LT);
       mbar_init(&q_empty[b], 1);
-      mbar_init(&k_full[b], kLoadThreads);
+      mbar_init(&k_full[b], LT);
       mbar_init(&k_empty[b], 1);
-      mbar_init(&v_full[b], kLoadThreads);
+      mbar_init(&v_full[b], LT);
       mbar_init(&v_empty[b], 1);
     }
     for (int g = 0; g < NWG; ++g) {
@@ -311,10 +319,10 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       pend = cur;
     }
     if (pend.any) finish(pend, false);
-  } else if (warp < 4 * NWG + kLoadWarps) {
+  } else if (warp < 4 * NWG + LT / 32) {
     // ================= loads =================
     const int lt = tid - 4 * NWG * 32;
-    Jobs jobs;
+    RowTables<LT> tab{s_rows, 0};
     uint32_t it = 0, qi = 0;  // key tiles and work items so far
     int hg = -1, hj = 0, hlo = 0, hcnt = 0;  // the keys that stay
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
@@ -329,44 +337,37 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       const T* vp = (const T*)a.v + k.g * a.vs.item + k.j * a.vs.head;
       auto key_tile = [&](const T* base, int64_t step, unsigned char* to, int k0) {
         const int n = min(kt, k.cnt - k0);
-        copy_tile<T>(smem_u32(to), (n + 15) & ~15, D, d16, base, lt, [&](int r) {
-          return r < n ? base + keys.at(k.g, k.lo + k0 + r) * step : (const T*)nullptr;
-        });
+        copy_keys<LT, T>(tab, smem_u32(to), base, step, keys, k.g, k.lo + k0, n, (n + 15) & ~15, D, d16, lt);
       };
       const uint32_t qb = qi % sh.qbufs;
       for (int k0 = 0; k0 < k.cnt; k0 += kt) {
         uint32_t st = it % sh.stages;
         if (!reuse) {
-          if (it >= (uint32_t)sh.stages) jobs.wait(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
+          if (it >= (uint32_t)sh.stages) wait_or_bad(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
           key_tile(kp, a.ks.token, sk + st * ktile, k0);
-          jobs.push(&k_full[st]);
+          copies_arrive(&k_full[st]);
         }
         if (k0 == 0) {
-          if (qi >= (uint32_t)sh.qbufs) jobs.wait(&q_empty[qb], (qi / sh.qbufs - 1) & 1u, bad, a.status);
+          if (qi >= (uint32_t)sh.qbufs) wait_or_bad(&q_empty[qb], (qi / sh.qbufs - 1) & 1u, bad, a.status);
           const T* qp = (const T*)a.q + k.n * a.qs.item + k.j * R * a.qs.head;
 #pragma unroll 1
           for (int g = 0; g < NWG; ++g) {
             const int tile = k.group * NWG + g;
-            if (tile < sh.tiles) {
-              const uint32_t m0 = (uint32_t)tile * 128;
-              copy_tile<T>(smem_u32(sq + (qb * NWG + g) * qtile), 128, D, d16, qp, lt, [&](int r) {
-                const uint32_t m = m0 + r, t = R == 1 ? m : m / (uint32_t)R;
-                return t < (uint32_t)a.Q ? qp + t * a.qs.token + (R == 1 ? 0 : (m - t * R) * a.qs.head) : (const T*)nullptr;
-              });
-            }
-            jobs.push(&q_full[qb][g]);
+            if (tile < sh.tiles)
+              copy_queries<LT, T>(tab, smem_u32(sq + (qb * NWG + g) * qtile), qp, a.qs, (uint32_t)tile * 128, R, a.Q, D, d16, lt);
+            copies_arrive(&q_full[qb][g]);
           }
         }
         if (!reuse) {
-          if (it >= (uint32_t)sh.stages) jobs.wait(&v_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
+          if (it >= (uint32_t)sh.stages) wait_or_bad(&v_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
           key_tile(vp, a.vs.token, sv + st * ktile, k0);
-          jobs.push(&v_full[st]);
+          copies_arrive(&v_full[st]);
           ++it;
         }
       }
       ++qi;
     }
-    jobs.flush();
+    copies_drain();
   } else if (lane == 0) {
     // ================= MMAs =================
     const uint32_t aq = smem_u32(sq), ak = smem_u32(sk), av = smem_u32(sv), step = (uint32_t)d16 * 32;  // 16 rows
@@ -382,7 +383,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       wait_or_bad(&p_full[g], (p_par >> g) & 1u, bad, a.status);
       p_par ^= 1u << g;
       if (!v_ready) {
-        wait_or_bad(&v_full[pst], (pit / sh.stages) & 1u, bad, a.status);
+        landed(&v_full[pst], (pit / sh.stages) & 1u, bad, a.status);
         v_ready = true;
       }
       tc_fence_after_sync();
@@ -408,7 +409,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         if (!reuse) {
           if (k0 == 0 && held) tc_commit(&k_empty[pst]);  // the keys that stayed are used up
           st = it % sh.stages;
-          wait_or_bad(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
+          landed(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
         }
         const uint32_t idesc = tc_idesc_16(128, n16, kBf16, 0, 0);
 #pragma unroll
@@ -416,7 +417,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
           if (pv[g]) second(g);
           pv[g] = k.group * NWG + g < sh.tiles;
           if (pv[g]) {
-            if (k0 == 0) wait_or_bad(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+            if (k0 == 0) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
             tc_fence_after_sync();
             const uint32_t tS = taddr + (uint32_t)g * (kt + d16);
             for (int ks = 0; ks < d16 / 16; ++ks)
@@ -456,7 +457,7 @@ struct TcPlan {
   size_t smem;
 };
 constexpr int kSms = 152;
-constexpr size_t kSmemMost = 224 << 10;
+constexpr size_t kSmemMost = 222 << 10;
 
 size_t tc_smem(int nwg, const TcShape& sh, int D) {
   const size_t row = (size_t)sh.d16 * 2;

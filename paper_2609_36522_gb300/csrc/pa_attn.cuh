@@ -70,67 +70,115 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
-// The loader threads' copies: a job is the copies behind one mbarrier. Up to
-// three jobs are in flight; a job's barrier gets each thread's arrival when the
-// thread's copies have landed and are visible to the tensor core.
-struct Jobs {
-  uint64_t *b0, *b1;
-  int n;
-  __device__ Jobs() : b0(nullptr), b1(nullptr), n(0) {}
-  __device__ __forceinline__ void push(uint64_t* bar) {
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    if (n == 2) {
-      asm volatile("cp.async.wait_group 2;" ::: "memory");
-      fence_proxy_async_smem();
-      mbar_arrive(b0);
-      b0 = b1;
-      b1 = bar;
-    } else {
-      if (n == 0) b0 = bar;
-      else b1 = bar;
-      ++n;
+// The loader threads' copies of a job land some time later; its mbarrier then
+// gets each thread's arrival. Whoever waits for them to issue MMAs makes them
+// visible to the tensor core (landed).
+__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void copies_drain() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void landed(uint64_t* bar, uint32_t parity, bool& bad, int32_t* status) {
+  wait_or_bad(bar, parity, bad, status);
+  fence_proxy_async_smem();
+}
+
+// Copy `rows` (a multiple of 8) rows of a tile by LT threads, zeros from row
+// `valid` on. Eight neighbouring threads fill a core matrix; neighbouring groups
+// of eight take neighbouring 16-byte pieces of the same eight rows. Rows at one
+// distance: pointers only ever step.
+template <int LT, typename T>
+__device__ __forceinline__ void copy_rows(uint32_t dst, int rows, int valid, int d, int d16, const T* base, int64_t stride,
+                                          int tid) {
+  const int nch = d >> 3;
+  int c = tid >> 3, row = tid & 7;
+  row += c / nch * 8;
+  c %= nch;
+  const T* p = base + row * stride + c * 8;
+  dst += (uint32_t)(row >> 3) * d16 * 16 + c * 128 + (row & 7) * 16;
+  const int dc = (LT / 8) % nch, dr = (LT / 8) / nch * 8;
+  const int64_t dp = dr * stride + dc * 8, wp = 8 * stride - nch * 8;
+  const uint32_t dd = (uint32_t)(dr >> 3) * d16 * 16 + dc * 128, wd = (uint32_t)d16 * 16 - nch * 128;
+#pragma unroll 4
+  while (row < rows) {
+    copy16(dst, row < valid ? p : base, row < valid);
+    c += dc;
+    row += dr;
+    p += dp;
+    dst += dd;
+    if (c >= nch) {
+      c -= nch;
+      row += 8;
+      p += wp;
+      dst += wd;
     }
   }
-  __device__ __forceinline__ void flush() {
-    if (n == 0) return;
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    fence_proxy_async_smem();
-    mbar_arrive(b0);
-    if (n == 2) mbar_arrive(b1);
-    n = 0;
+}
+// Rows at offsets (in elements, negative: zeros) that a table in shared memory holds.
+template <int LT, typename T>
+__device__ __forceinline__ void copy_rows_at(uint32_t dst, int rows, int d, int d16, const T* base, const int64_t* off, int tid) {
+  const int nch = d >> 3;
+  int c = tid >> 3, row = tid & 7;
+  row += c / nch * 8;
+  c %= nch;
+  dst += (uint32_t)(row >> 3) * d16 * 16 + c * 128 + (row & 7) * 16;
+  const int dc = (LT / 8) % nch, dr = (LT / 8) / nch * 8;
+  const uint32_t dd = (uint32_t)(dr >> 3) * d16 * 16 + dc * 128, wd = (uint32_t)d16 * 16 - nch * 128;
+#pragma unroll 4
+  while (row < rows) {
+    const int64_t o = off[row];
+    copy16(dst, base + (o < 0 ? 0 : o + c * 8), o >= 0);
+    c += dc;
+    row += dr;
+    dst += dd;
+    if (c >= nch) {
+      c -= nch;
+      row += 8;
+      dst += wd;
+    }
   }
-  // A wait of a loader: what others wait for comes first.
-  __device__ __forceinline__ void wait(uint64_t* bar, uint32_t parity, bool& bad, int32_t* status) {
-    if (!bad && mbar_test(bar, parity)) return;
-    flush();
-    wait_or_bad(bar, parity, bad, status);
+}
+
+// What the loader threads share: a table of row offsets, two in turn (a thread
+// that fills one has seen every thread pass the barrier after the other's use).
+template <int LT>
+struct RowTables {
+  int64_t (*at)[128];
+  int turn;
+  // off(r): element offset of row r, negative: zeros
+  template <typename F>
+  __device__ __forceinline__ const int64_t* fill(int rows, int tid, F off) {
+    int64_t* t = at[turn ^= 1];
+    for (int r = tid; r < rows; r += LT) t[r] = off(r);
+    asm volatile("bar.sync 1, %0;" ::"n"(LT) : "memory");
+    return t;
   }
 };
 
-constexpr int kLoadWarps = 3;  // with the warp that issues the MMAs a multiple of four: registers go by four warps
-constexpr int kLoadThreads = kLoadWarps * 32;
-
-// Copy `rows` (a multiple of 8) rows of a tile: row r from at(r), zeros where at
-// gives NULL. `any`: an address that may be named. By kLoadThreads threads.
-template <typename T, typename At>
-__device__ __forceinline__ void copy_tile(uint32_t dst, int rows, int d, int d16, const T* any, int tid, At at) {
-  const int nch = d >> 3, r = tid & 7;
-  int c = tid >> 3, rg = 0;
-  while (c >= nch) {
-    c -= nch;
-    ++rg;
+// Rows m0 .. m0 + 127 of an item and key head (m = token x R + head of the key
+// head), zeros past the last token; keys k0 .. k0 + n - 1 of a source's keys
+// that count, zeros up to a multiple of 16.
+template <int LT, typename T>
+__device__ __forceinline__ void copy_queries(RowTables<LT>& tab, uint32_t dst, const T* base, const Strides& s, uint32_t m0,
+                                             int R, int Q, int d, int d16, int tid) {
+  if (R == 1) {
+    copy_rows<LT, T>(dst, 128, min(128, Q - (int)m0), d, d16, base + m0 * s.token, s.token, tid);
+    return;
   }
-  const int dc = (kLoadThreads / 8) % nch, dg = (kLoadThreads / 8) / nch;
-  for (; rg * 8 < rows;) {
-    const T* p = at(rg * 8 + r);
-    copy16(dst + (uint32_t)(rg * (d16 >> 3) + c) * 128 + r * 16, p ? p + c * 8 : any, p != nullptr);
-    c += dc;
-    rg += dg;
-    if (c >= nch) {
-      c -= nch;
-      ++rg;
-    }
+  const int64_t* off = tab.fill(128, tid, [&](int r) {
+    const uint32_t m = m0 + r, t = m / (uint32_t)R;
+    return t < (uint32_t)Q ? t * s.token + (m - t * R) * s.head : (int64_t)-1;
+  });
+  copy_rows_at<LT, T>(dst, 128, d, d16, base, off, tid);
+}
+template <int LT, typename T>
+__device__ __forceinline__ void copy_keys(RowTables<LT>& tab, uint32_t dst, const T* base, int64_t stride, const Keys& keys, int g,
+                                          int k0, int n, int rows, int d, int d16, int tid) {
+  if (!keys.list) {
+    copy_rows<LT, T>(dst, rows, n, d, d16, base + k0 * stride, stride, tid);
+    return;
   }
+  const int64_t* off = tab.fill(rows, tid, [&](int r) { return r < n ? keys.at(g, k0 + r) * stride : (int64_t)-1; });
+  copy_rows_at<LT, T>(dst, rows, d, d16, base, off, tid);
 }
 
 // The list above (k_attn.cu).

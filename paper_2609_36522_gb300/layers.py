@@ -11,27 +11,33 @@ give ``count`` (the device address of the miss count), the output buffers and
 """
 from __future__ import annotations
 
+import struct
+
 import torch
 
 from . import abi
 
 _DTYPES = {torch.float32: abi.PA_F32, torch.float16: abi.PA_F16, torch.bfloat16: abi.PA_BF16}
+_HALVES = (torch.float16, torch.bfloat16)
+_raw_stream = torch._C._cuda_getCurrentRawStream  # the current stream's address, without an object around it
+
+# The checks below are on the critical path of small calls, which take less time
+# on the GPU than here: no message is put together unless it is raised.
 
 
-def _on(x, stream):
-    """The stream's address; allocations must be made with that stream current."""
-    if stream is None:
-        stream = torch.cuda.current_stream(x.device)
-    return stream.cuda_stream
+class _Here:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
 
 
-class _Place:
-    """The tensors' device and the given stream as the current ones."""
+class _There:
+    """A tensor's device and a stream as the current ones."""
 
-    def __init__(self, x, stream):
-        self.guards = []
-        if x.device.index != torch.cuda.current_device():
-            self.guards.append(torch.cuda.device(x.device))
+    def __init__(self, device, stream):
+        self.guards = [torch.cuda.device(device)]
         if stream is not None:
             self.guards.append(torch.cuda.stream(stream))
 
@@ -44,13 +50,19 @@ class _Place:
             g.__exit__(*exc)
 
 
-def _check(ok, what):
-    if not ok:
-        raise ValueError(what)
+_here = _Here()
+
+
+def _place(x, stream):
+    """Where a call on x allocates and launches."""
+    if stream is None and x.get_device() == torch.cuda.current_device():
+        return _here
+    return _There(x.device, stream)
 
 
 def _device(name, t, like):
-    _check(isinstance(t, torch.Tensor) and t.is_cuda and t.device == like.device, f"{name} must be a tensor on x's GPU")
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() == like.get_device()):
+        raise ValueError(f"{name} must be a tensor on the GPU of what it belongs to")
 
 
 def _count(count, like):
@@ -58,18 +70,21 @@ def _count(count, like):
     if count is None or isinstance(count, int):
         return count
     _device("count", count, like)
-    _check(count.dtype == torch.int32 and count.numel() == 1, "count must be one int32 on the device")
+    if count.dtype != torch.int32 or count.numel() != 1:
+        raise ValueError("count must be one int32 on the device")
     return count.data_ptr()
 
 
 def _workspace(workspace, need, like):
+    """-> (address, bytes, what keeps it alive until the call is enqueued)"""
     if need == 0:
         return None, 0, None
     if workspace is None:
         workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
-    else:
-        _device("workspace", workspace, like)
-        _check(workspace.is_contiguous(), "workspace must be contiguous")
+        return workspace.data_ptr(), need, workspace
+    _device("workspace", workspace, like)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
@@ -77,34 +92,52 @@ def _workspace(workspace, need, like):
 
 def _rows(name, x, like=None):
     """(rows, row stride) of a tensor [..., cols] whose rows lie at one distance."""
-    _check(isinstance(x, torch.Tensor) and x.is_cuda and x.dim() >= 1, f"{name} must be a CUDA tensor")
-    if like is not None:
-        _check(x.shape == like.shape and x.dtype == like.dtype and x.device == like.device,
-               f"{name} must have x's shape, type and device")
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() >= 1):
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if like is not None and not (x.shape == like.shape and x.dtype == like.dtype and x.get_device() == like.get_device()):
+        raise ValueError(f"{name} must have x's shape, type and device")
     cols = x.shape[-1]
     if x.is_contiguous():
         return x.numel() // cols if cols else 0, cols
-    _check(x.stride(-1) == 1 or cols == 1, f"{name}'s last axis must be contiguous")
+    if x.stride(-1) != 1 and cols != 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
     rows, step = 1, None
     for n, s in zip(reversed(x.shape[:-1]), reversed(x.stride()[:-1])):
         if n == 1:
             continue
-        _check(step is None or s == step * rows, f"{name}'s rows must lie at one distance")
+        if step is not None and s != step * rows:
+            raise ValueError(f"{name}'s rows must lie at one distance")
         step = s if step is None else step
         rows *= n
     return rows, cols if step is None else step
 
 
-def _weights(x, **named):
-    for name, w in named.items():
-        if w is not None:
-            _device(name, w, x)
-            _check(w.dtype == x.dtype and w.is_contiguous() and w.shape == x.shape[-1:],
-                   f"{name} must be contiguous, of x's type and last size")
+def _weight(name, w, x):
+    """The address of a weight or bias of x's last axis."""
+    if w is None:
+        return None
+    _device(name, w, x)
+    if not (w.dtype == x.dtype and w.is_contiguous() and w.dim() == 1 and w.shape[0] == x.shape[-1]):
+        raise ValueError(f"{name} must be contiguous, of x's type and last size")
+    return w.data_ptr()
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+def _stat(name, t, x):
+    _device(name, t, x)
+    if not (t.dtype == torch.float32 and t.is_contiguous() and t.shape == x.shape[:-1]):
+        raise ValueError(f"{name} must be contiguous float32 of x's shape without the last axis")
+    return t.data_ptr()
+
+
+def _dtype(x):
+    dtype = _DTYPES.get(x.dtype)
+    if dtype is None:
+        raise ValueError("x must be float32, float16 or bfloat16")
+    return dtype
+
+
+def _per_item(x, rows):
+    return max(1, rows // x.shape[0]) if x.dim() > 1 and x.shape[0] else 1
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, stats=False, out=None, mean=None, rstd=None, count=None, stream=None):
@@ -114,33 +147,24 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, stats=False, out=None, mean=
     ``out``: where y goes (x itself is allowed). ``count``: device int32, only
     the first ``count`` entries of x's first axis are computed."""
     rows, xs = _rows("x", x)
-    _check(x.dtype in _DTYPES, "x must be float32, float16 or bfloat16")
-    _weights(x, weight=weight, bias=bias)
-    with _Place(x, stream):
+    dtype = _dtype(x)
+    w, b = _weight("weight", weight, x), _weight("bias", bias, x)
+    with _place(x, stream):
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        _, ys = _rows("out", out, x)
+            out, ys = (torch.empty_like(x), xs) if x.is_contiguous() else (torch.empty(x.shape, dtype=x.dtype, device=x.device),
+                                                                          x.shape[-1])
+        else:
+            _, ys = _rows("out", out, x)
+        mp = rp = None
         if stats or mean is not None or rstd is not None:
             if mean is None:
                 mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
             if rstd is None:
                 rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-            _stats(x, mean, rstd)
-        abi.pa_layer_norm(_DTYPES[x.dtype], rows, x.shape[-1], x.data_ptr(), xs, _ptr(weight), _ptr(bias), eps,
-                          out.data_ptr(), ys, _ptr(mean), _ptr(rstd), _count(count, x),
-                          _per_item(x, rows), _on(x, stream))
+            mp, rp = _stat("mean", mean, x), _stat("rstd", rstd, x)
+        abi.pa_layer_norm(dtype, rows, x.shape[-1], x.data_ptr(), xs, w, b, eps, out.data_ptr(), ys, mp, rp,
+                          _count(count, x), _per_item(x, rows), _raw_stream(x.get_device()))
     return out if mean is None else (out, mean, rstd)
-
-
-def _per_item(x, rows):
-    return max(1, rows // x.shape[0]) if x.dim() > 1 and x.shape[0] else 1
-
-
-def _stats(x, mean, rstd):
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _device(name, t, x)
-        _check(t.dtype == torch.float32 and t.is_contiguous() and t.shape == x.shape[:-1],
-               f"{name} must be contiguous float32 of x's shape without the last axis")
 
 
 def layer_norm_backward(dy, x, mean, rstd, weight=None, weight_grad=True, bias_grad=True, dx=None, count=None,
@@ -151,70 +175,82 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, weight_grad=True, bias_g
     ``workspace``: a CUDA tensor of at least
     ``abi.pa_layer_norm_backward_workspace_bytes(rows, cols)`` bytes."""
     rows, xs = _rows("x", x)
-    _check(x.dtype in _DTYPES, "x must be float32, float16 or bfloat16")
+    dtype, cols = _dtype(x), x.shape[-1]
     _, dys = _rows("dy", dy, x)
-    _weights(x, weight=weight)
-    _stats(x, mean, rstd)
-    cols = x.shape[-1]
-    with _Place(x, stream):
+    w, mp, rp = _weight("weight", weight, x), _stat("mean", mean, x), _stat("rstd", rstd, x)
+    with _place(x, stream):
         if dx is None:
             dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        _, dxs = _rows("dx", dx, x)
+            dxs = cols
+        else:
+            _, dxs = _rows("dx", dx, x)
         dw = torch.empty(cols, dtype=x.dtype, device=x.device) if weight_grad else None
         db = torch.empty(cols, dtype=x.dtype, device=x.device) if bias_grad else None
         need = abi.pa_layer_norm_backward_workspace_bytes(rows, cols) if weight_grad or bias_grad else 0
         ws, nbytes, keep = _workspace(workspace, need, x)
-        abi.pa_layer_norm_backward(_DTYPES[x.dtype], rows, cols, dy.data_ptr(), dys, x.data_ptr(), xs, _ptr(weight),
-                                   mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dxs, _ptr(dw), _ptr(db),
-                                   _count(count, x), _per_item(x, rows), ws, nbytes, _on(x, stream))
+        abi.pa_layer_norm_backward(dtype, rows, cols, dy.data_ptr(), dys, x.data_ptr(), xs, w, mp, rp, dx.data_ptr(), dxs,
+                                   None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),
+                                   _count(count, x), _per_item(x, rows), ws, nbytes, _raw_stream(x.get_device()))
     return dx, dw, db
 
 
 # ---- cross attention --------------------------------------------------------------
 
-def _arguments(q, k, v, scale, source, lengths, mask, count):
-    """The argument block's first part: what both directions share."""
+_BLOCK = struct.Struct("=8id3Q9qQqQQqQQ3qQ4Q12q")  # pa_attention_t
+_NO_GRADIENTS = (0,) * 16
+
+
+def _tensor(name, t, like=None):
+    """(address, strides) of a tensor [a][b][c][d] whose last axis is contiguous.
+    An axis of one entry has no stride that matters (torch leaves any value there)."""
+    if like is not None and not (isinstance(t, torch.Tensor) and t.shape == like.shape and t.dtype == like.dtype
+                                 and t.get_device() == like.get_device()):
+        raise ValueError(f"{name} must have the shape, type and device of what it belongs to")
+    (n0, n1, n2, n3), (s0, s1, s2, s3) = t.shape, t.stride()
+    if s3 != 1 and n3 != 1:
+        raise ValueError(f"{name}'s last axis must be contiguous")
+    return t.data_ptr(), (s0 if n0 > 1 else 0, s1 if n1 > 1 else 0, s2 if n2 > 1 else 0)
+
+
+def _inputs(q, k, v, scale, source, lengths, mask, count):
+    """The argument block up to n_items_dev: what both directions share."""
     for name, t in (("q", q), ("k", k), ("v", v)):
-        _check(isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 4, f"{name} must be a CUDA tensor of four axes")
-        _check(t.dtype == q.dtype and t.device == q.device, f"{name} must have q's type and device")
-    _check(q.dtype in (torch.float16, torch.bfloat16), "q, k and v must be float16 or bfloat16")
-    _check(k.shape == v.shape and k.shape[3] == q.shape[3], "k and v need one shape, and q's last size")
-    a = abi.PaAttention()
-    a.dtype = _DTYPES[q.dtype]
-    a.items, a.tokens, a.heads, a.head_dim = q.shape
-    a.sources, a.keys, a.kv_heads = k.shape[:3]
-    a.scale = q.shape[3] ** -0.5 if scale is None else scale
-    a.q, a.q_stride = _tensor("q", q)
-    a.k, a.k_stride = _tensor("k", k)
-    a.v, a.v_stride = _tensor("v", v)
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 4):
+            raise ValueError(f"{name} must be a CUDA tensor of four axes")
+    if not (q.dtype == k.dtype == v.dtype and q.get_device() == k.get_device() == v.get_device()):
+        raise ValueError("q, k and v must have one type and device")
+    if q.dtype not in _HALVES:
+        raise ValueError("q, k and v must be float16 or bfloat16")
+    if k.shape != v.shape or k.shape[3] != q.shape[3]:
+        raise ValueError("k and v need one shape, and q's last size")
+    items, tokens, heads, dim = q.shape
+    sources, keys, kv_heads, _ = k.shape
+    (qp, qs), (kp, ks), (vp, vs) = _tensor("q", q), _tensor("k", k), _tensor("v", v)
+    sp = ss = lp = mp = ms = 0
     if source is not None:
         _device("source", source, q)
-        _check(source.dtype == torch.int32 and source.dim() == 1 and source.shape[0] >= q.shape[0],
-               "source must be an int32 vector with an entry per item")
-        a.source, a.source_stride = source.data_ptr(), source.stride(0)
+        if source.dtype != torch.int32 or source.dim() != 1 or source.shape[0] < items:
+            raise ValueError("source must be an int32 vector with an entry per item")
+        sp, ss = source.data_ptr(), source.stride(0)
     if lengths is not None:
         _device("lengths", lengths, q)
-        _check(lengths.dtype == torch.int32 and lengths.is_contiguous() and lengths.shape == k.shape[:1],
-               "lengths must be a contiguous int32 vector with an entry per source")
-        a.lengths = lengths.data_ptr()
+        if lengths.dtype != torch.int32 or not lengths.is_contiguous() or lengths.shape != (sources,):
+            raise ValueError("lengths must be a contiguous int32 vector with an entry per source")
+        lp = lengths.data_ptr()
     if mask is not None:
         _device("mask", mask, q)
-        _check(mask.dtype in (torch.bool, torch.uint8) and mask.shape == k.shape[:2]
-               and (mask.stride(1) == 1 or mask.shape[1] <= 1),
-               "mask must be bool or uint8 [sources][keys], its last axis contiguous")
-        a.mask, a.mask_stride = mask.data_ptr() or None, mask.stride(0)
-    a.n_items_dev = _count(count, q)
-    return a
+        if not (mask.dtype in (torch.bool, torch.uint8) and mask.shape == (sources, keys) and (mask.stride(1) == 1 or keys <= 1)):
+            raise ValueError("mask must be bool or uint8 [sources][keys], its last axis contiguous")
+        mp, ms = mask.data_ptr(), mask.stride(0)
+    return (_DTYPES[q.dtype], items, tokens, sources, keys, heads, kv_heads, dim, (dim or 1) ** -0.5 if scale is None else scale,
+            qp, kp, vp, *qs, *ks, *vs, sp, ss, lp, mp, ms, _count(count, q) or 0)
 
 
-# an axis of one entry has no stride that matters (torch leaves any value there)
-def _tensor(name, t, like=None):
-    if like is not None:
-        _check(isinstance(t, torch.Tensor) and t.is_cuda and t.shape == like.shape and t.dtype == like.dtype
-               and t.device == like.device, f"{name} must have the shape, type and device of what it belongs to")
-    shape, s = t.shape, t.stride()
-    _check(s[3] == 1 or shape[3] == 1, f"{name}'s last axis must be contiguous")
-    return t.data_ptr(), (s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0, s[2] if shape[2] > 1 else 0)
+def _lse(lse, q):
+    _device("lse", lse, q)
+    if not (lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:3]):
+        raise ValueError("lse must be contiguous float32 [items][tokens][heads]")
+    return lse.data_ptr()
 
 
 def cross_attention(q, k, v, scale=None, source=None, lengths=None, mask=None, count=None, stats=False, out=None, lse=None,
@@ -231,25 +267,17 @@ def cross_attention(q, k, v, scale=None, source=None, lengths=None, mask=None, c
     items are computed. Returns out, with ``stats`` (or a buffer ``lse``)
     (out, lse) for ``cross_attention_backward``: lse float32 [items][tokens][heads].
     ``workspace``: a CUDA tensor, see ``cross_attention_workspace_bytes``."""
-    a = _arguments(q, k, v, scale, source, lengths, mask, count)
-    with _Place(q, stream):
+    given = _inputs(q, k, v, scale, source, lengths, mask, count)
+    with _place(q, stream):
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        a.out, a.out_stride = _tensor("out", out, q)
+        op, os = _tensor("out", out, q)
         if stats and lse is None:
             lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
-        if lse is not None:
-            _lse(lse, q)
-            a.lse = lse.data_ptr()
-        ws, nbytes, keep = _workspace(workspace, abi.pa_attention_workspace_bytes(a, 0), q)
-        abi.pa_attention(a, ws, nbytes, _on(q, stream))
+        block = _BLOCK.pack(*given, op, *os, 0 if lse is None else _lse(lse, q), *_NO_GRADIENTS)
+        ws, nbytes, keep = _workspace(workspace, abi.pa_attention_workspace_bytes(block, 0), q)
+        abi.pa_attention(block, ws, nbytes, _raw_stream(q.get_device()))
     return out if lse is None else (out, lse)
-
-
-def _lse(lse, q):
-    _device("lse", lse, q)
-    _check(lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:3],
-           "lse must be contiguous float32 [items][tokens][heads]")
 
 
 def cross_attention_backward(dout, q, k, v, out, lse, scale=None, source=None, lengths=None, mask=None, count=None,
@@ -257,31 +285,26 @@ def cross_attention_backward(dout, q, k, v, out, lse, scale=None, source=None, l
     """Gradients of ``cross_attention`` for dout: (dq, dk, dv). The arguments and
     out and lse are the forward call's; dk and dv are sums over all rows that
     attend to a source, and zero for keys that do not count."""
-    a = _arguments(q, k, v, scale, source, lengths, mask, count)
-    a.out, a.out_stride = _tensor("out", out, q)
-    a.dout, a.dout_stride = _tensor("dout", dout, q)
-    _lse(lse, q)
-    a.lse = lse.data_ptr()
-    with _Place(q, stream):
+    given = _inputs(q, k, v, scale, source, lengths, mask, count)
+    (op, os), (gp, gs) = _tensor("out", out, q), _tensor("dout", dout, q)
+    lp = _lse(lse, q)
+    with _place(q, stream):
         dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
         dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
         dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if dv is None else dv
-        a.dq, a.dq_stride = _tensor("dq", dq, q)
-        a.dk, a.dk_stride = _tensor("dk", dk, k)
-        a.dv, a.dv_stride = _tensor("dv", dv, v)
-        ws, nbytes, keep = _workspace(workspace, abi.pa_attention_workspace_bytes(a, 1), q)
-        abi.pa_attention_backward(a, ws, nbytes, _on(q, stream))
+        (qp, qs), (kp, ks), (vp, vs) = _tensor("dq", dq, q), _tensor("dk", dk, k), _tensor("dv", dv, v)
+        block = _BLOCK.pack(*given, op, *os, lp, gp, qp, kp, vp, *gs, *qs, *ks, *vs)
+        ws, nbytes, keep = _workspace(workspace, abi.pa_attention_workspace_bytes(block, 1), q)
+        abi.pa_attention_backward(block, ws, nbytes, _raw_stream(q.get_device()))
     return dq, dk, dv
 
 
 def cross_attention_workspace_bytes(q, k, mask=False, backward=False):
     """Bytes of workspace of a call on tensors of these shapes."""
-    a = abi.PaAttention()
-    a.dtype = abi.PA_BF16
-    a.items, a.tokens, a.heads, a.head_dim = q.shape
-    a.sources, a.keys, a.kv_heads = k.shape[:3]
-    a.mask = 1 if mask else None
-    return abi.pa_attention_workspace_bytes(a, backward)
+    (items, tokens, heads, dim), (sources, keys, kv_heads) = q.shape, k.shape[:3]
+    block = _BLOCK.pack(abi.PA_BF16, items, tokens, sources, keys, heads, kv_heads, dim, 1.0, *(0,) * 15, int(mask), 0, 0,
+                        *(0,) * 5, *_NO_GRADIENTS)
+    return abi.pa_attention_workspace_bytes(block, backward)
 
 
 def check(stream=None):
