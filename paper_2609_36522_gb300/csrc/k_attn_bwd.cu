@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
   __shared__ uint32_t s_taddr;
   __shared__ int2 s_work[kTable];
   __shared__ int64_t s_rows[2][128];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
   const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2, cols = 2 * kt + d16;
   unsigned char* sq = smem;                                 // per buffer and group: q, dout
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
   }
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t taddr = s_taddr;
+  const uint32_t taddr = uniform(s_taddr);
   pdl_wait();
   pdl_trigger();
   const int works = items_of(a.count, a.N) * sh.groups * a.J;
@@ -138,7 +138,9 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
   __syncthreads();
   auto work = [&](int i, int w) {
     Work k;
-    const int2 f = i < kTable ? s_work[i] : look(w);
+    int2 f = i < kTable ? s_work[i] : look(w);
+    f.x = uniform(f.x);
+    f.y = uniform(f.y);
     k.g = f.x;
     k.cnt = f.y;
     k.j = w % a.J;
@@ -310,9 +312,11 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
       ++qi;
     }
     copies_drain();
-  } else if (lane == 0) {
+  } else {
     // ================= MMAs =================
-    const uint32_t aq = smem_u32(sq), ak = smem_u32(sk), step = (uint32_t)d16 * 32;
+    const uint64_t dq0 = tile_desc_rows(smem_u32(sq), d16), dk0 = tile_desc_rows(smem_u32(sk), d16),
+                   dc0 = tile_desc_cols(smem_u32(sk), d16);
+    const uint32_t uq = qtile / 16, uk = ktile / 16, idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
     uint32_t it = 0, qi = 0, p_par = 0;
     int hg = -1, hj = 0;
     bool pv[NWG], plast = false, pfirst = false, pmul = false, have = false;
@@ -323,13 +327,14 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
     auto second = [&](int g) {  // the step before is taken; dQ += dS K in the second sweep
       wait_or_bad(&p_full[g], (p_par >> g) & 1u, bad, a.status);
       p_par ^= 1u << g;
+      __syncwarp();
       tc_fence_after_sync();
       if (!pmul) return;
-      const uint32_t tS = taddr + (uint32_t)g * cols, idesc = tc_idesc_16(128, d16, kBf16, 0, 1);
-      for (int ks = 0; ks < pn16 / 16; ++ks)
-        tc_mma_f16_ta(tS + 2 * kt, tS + ks * 8, tile_desc_cols(ak + pst * 2 * ktile + ks * step, d16), idesc,
-                      !pfirst || ks > 0 ? 1u : 0u);
-      if (plast) tc_commit(&o_full[g]);
+      const uint32_t tS = taddr + (uint32_t)g * cols;
+      if (elect_one()) {
+        mma_steps_ta(tS + 2 * kt, tS, dc0 + pst * 2 * uk, d16 * 2, pn16 / 16, idesc2, !pfirst);
+        if (plast) tc_commit(&o_full[g]);
+      }
     };
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
       const Work k = work(i, w);
@@ -352,7 +357,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
                   second(g);
                   pv[g] = false;
                 }
-              tc_commit(&k_empty[pst]);
+              if (elect_one()) tc_commit(&k_empty[pst]);
             }
             landed(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
           }
@@ -364,17 +369,18 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
             pv[g] = k.group * NWG + g < sh.tiles;
             if (pv[g]) {
               if (firsts) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+              __syncwarp();
               tc_fence_after_sync();
-              const uint32_t tS = taddr + (uint32_t)g * cols, q = aq + (qb * NWG + g) * 2 * qtile, kk = ak + st * 2 * ktile;
-              for (int ks = 0; ks < d16 / 16; ++ks)
-                tc_mma_f16(tS, tile_desc_rows(q + ks * 256, d16), tile_desc_rows(kk + ks * 256, d16), idesc, ks > 0 ? 1u : 0u);
-              for (int ks = 0; ks < d16 / 16; ++ks)
-                tc_mma_f16(tS + kt, tile_desc_rows(q + qtile + ks * 256, d16), tile_desc_rows(kk + ktile + ks * 256, d16),
-                           idesc, ks > 0 ? 1u : 0u);
-              tc_commit(&s_full[g]);
+              if (elect_one()) {
+                const uint32_t tS = taddr + (uint32_t)g * cols;
+                const uint64_t q = dq0 + (qb * NWG + g) * 2 * uq, kk = dk0 + st * 2 * uk;
+                mma_steps(tS, q, 16, kk, 16, d16 / 16, idesc, false);
+                mma_steps(tS + kt, q + uq, 16, kk + uk, 16, d16 / 16, idesc, false);
+                tc_commit(&s_full[g]);
+              }
             }
           }
-          if (have && !reuse && sh.stages > 1) tc_commit(&k_empty[pst]);
+          if (have && !reuse && sh.stages > 1 && elect_one()) tc_commit(&k_empty[pst]);
           have = true;
           if (!reuse) ++it;
           pst = st;
@@ -384,7 +390,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
           plast = sweep == 1 && k0 + kt >= k.cnt;
         }
       }
-      tc_commit(&q_empty[qb]);
+      if (elect_one()) tc_commit(&q_empty[qb]);
       ++qi;
     }
 #pragma unroll
@@ -417,7 +423,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
   __shared__ uint32_t s_taddr;
   __shared__ __align__(16) float2 s_stat[kDkvStages][64];
   __shared__ int64_t s_off[2][2][64], s_rows[2][128];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, qt = sh.qt, rows_item = a.Q * R;
   pdl_wait();
   int b = blockIdx.x;
@@ -468,7 +474,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
   }
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t taddr = s_taddr;
+  const uint32_t taddr = uniform(s_taddr);
   pdl_trigger();
   bool bad = false;
   const uint32_t acc = taddr + 4 * qt;  // dv, then dk
@@ -568,39 +574,42 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
       copies_arrive(&q_full[st]);
     }
     copies_drain();
-  } else if (lane == 0 && tiles > 0) {
+  } else if (tiles > 0) {
     // ================= MMAs =================
-    const uint32_t ak = smem_u32(sk), av = smem_u32(sv), aq = smem_u32(sq), step = (uint32_t)d16 * 32;
+    const uint64_t dk0 = tile_desc_rows(smem_u32(sk), d16), dv0 = tile_desc_rows(smem_u32(sv), d16),
+                   dq0 = tile_desc_rows(smem_u32(sq), d16), dc0 = tile_desc_cols(smem_u32(sq), d16);
+    const uint32_t uq = qtile / 16, uc = d16 * 2;
     const uint32_t idesc = tc_idesc_16(128, qt, kBf16, 0, 0), idesc2 = tc_idesc_16(128, dn, kBf16, 0, 1);
     uint32_t p_par = 0;
     landed(&k_full, 0, bad, a.status);
     auto scores = [&](int i) {
-      const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt, q = aq + st * 2 * qtile;
+      const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt;
       landed(&q_full[st], (i / sh.stages) & 1u, bad, a.status);
+      __syncwarp();
       tc_fence_after_sync();
-      for (int ks = 0; ks < d16 / 16; ++ks)
-        tc_mma_f16(tS, tile_desc_rows(ak + ks * 256, d16), tile_desc_rows(q + ks * 256, d16), idesc, ks > 0 ? 1u : 0u);
-      for (int ks = 0; ks < d16 / 16; ++ks)
-        tc_mma_f16(tS + qt, tile_desc_rows(av + ks * 256, d16), tile_desc_rows(q + qtile + ks * 256, d16), idesc,
-                   ks > 0 ? 1u : 0u);
-      tc_commit(&s_full[s]);
+      if (elect_one()) {
+        mma_steps(tS, dk0, 16, dq0 + st * 2 * uq, 16, d16 / 16, idesc, false);
+        mma_steps(tS + qt, dv0, 16, dq0 + (st * 2 + 1) * uq, 16, d16 / 16, idesc, false);
+        tc_commit(&s_full[s]);
+      }
     };
     scores(0);
     if (tiles > 1) scores(1);
     for (int i = 0; i < tiles; ++i) {
-      const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt, q = aq + st * 2 * qtile;
+      const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt;
       wait_or_bad(&p_full[s], (p_par >> s) & 1u, bad, a.status);
       p_par ^= 1u << s;
+      __syncwarp();
       tc_fence_after_sync();
-      for (int ks = 0; ks < qt / 16; ++ks)
-        tc_mma_f16_ta(acc, tS + ks * 8, tile_desc_cols(q + qtile + ks * step + c0 * 16, d16), idesc2, i > 0 || ks > 0 ? 1u : 0u);
-      for (int ks = 0; ks < qt / 16; ++ks)
-        tc_mma_f16_ta(acc + dn, tS + qt + ks * 8, tile_desc_cols(q + ks * step + c0 * 16, d16), idesc2,
-                      i > 0 || ks > 0 ? 1u : 0u);
-      tc_commit(&q_empty[st]);
+      if (elect_one()) {
+        const uint64_t q = dc0 + st * 2 * uq + c0;  // c0 columns: c0 / 8 core matrices of 128 bytes
+        mma_steps_ta(acc, tS, q + uq, uc, qt / 16, idesc2, i > 0);
+        mma_steps_ta(acc + dn, tS + qt, q, uc, qt / 16, idesc2, i > 0);
+        tc_commit(&q_empty[st]);
+      }
       if (i + 2 < tiles) scores(i + 2);
     }
-    tc_commit(&done);
+    if (elect_one()) tc_commit(&done);
   }
   __syncthreads();
   __syncwarp();

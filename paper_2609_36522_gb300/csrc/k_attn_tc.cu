@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   __shared__ uint32_t s_taddr;
   __shared__ int2 s_work[kTable];
   __shared__ int64_t s_rows[2][128];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
   const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2;
   unsigned char* sq = smem;
@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   }
   __syncthreads();
   tc_fence_after_sync();
-  const uint32_t taddr = s_taddr;
+  const uint32_t taddr = uniform(s_taddr);
   pdl_wait();
   pdl_trigger();
   const int works = items_of(a.count, a.N) * sh.groups * a.J * sh.splits;
@@ -115,7 +115,9 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   __syncthreads();
   auto work = [&](int i, int w) {
     Work k;
-    const int2 f = i < kTable ? s_work[i] : look(w);
+    int2 f = i < kTable ? s_work[i] : look(w);
+    f.x = uniform(f.x);
+    f.y = uniform(f.y);
     k.g = f.x;
     k.part = sh.splits > 1 ? w % sh.splits : 0;
     w /= sh.splits;
@@ -368,9 +370,11 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       ++qi;
     }
     copies_drain();
-  } else if (lane == 0) {
+  } else {
     // ================= MMAs =================
-    const uint32_t aq = smem_u32(sq), ak = smem_u32(sk), av = smem_u32(sv), step = (uint32_t)d16 * 32;  // 16 rows
+    const uint64_t dq0 = tile_desc_rows(smem_u32(sq), d16), dk0 = tile_desc_rows(smem_u32(sk), d16),
+                   dv0 = tile_desc_cols(smem_u32(sv), d16);
+    const uint32_t uq = qtile / 16, uk = ktile / 16, idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
     uint32_t it = 0, qi = 0, p_par = 0;  // p_par: a bit per group
     int hg = -1, hj = 0, hlo = 0, hcnt = 0;
     // the step whose O += P V are still to come
@@ -386,12 +390,13 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         landed(&v_full[pst], (pit / sh.stages) & 1u, bad, a.status);
         v_ready = true;
       }
+      __syncwarp();
       tc_fence_after_sync();
-      const uint32_t tS = taddr + (uint32_t)g * (kt + d16), idesc = tc_idesc_16(128, d16, kBf16, 0, 1);
-      for (int ks = 0; ks < pn16 / 16; ++ks)
-        tc_mma_f16_ta(tS + kt, tS + ks * 8, tile_desc_cols(av + pst * ktile + ks * step, d16), idesc,
-                      !pfirst || ks > 0 ? 1u : 0u);
-      if (plast) tc_commit(&o_full[g]);
+      const uint32_t tS = taddr + (uint32_t)g * (kt + d16);
+      if (elect_one()) {
+        mma_steps_ta(tS + kt, tS, dv0 + pst * uk, d16 * 2, pn16 / 16, idesc2, !pfirst);
+        if (plast) tc_commit(&o_full[g]);
+      }
     };
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
       const Work k = work(i, w);
@@ -407,7 +412,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         const int n16 = (min(kt, k.cnt - k0) + 15) & ~15;
         uint32_t st = pst;
         if (!reuse) {
-          if (k0 == 0 && held) tc_commit(&k_empty[pst]);  // the keys that stayed are used up
+          if (k0 == 0 && held && elect_one()) tc_commit(&k_empty[pst]);  // the keys that stayed are used up
           st = it % sh.stages;
           landed(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
         }
@@ -418,16 +423,18 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
           pv[g] = k.group * NWG + g < sh.tiles;
           if (pv[g]) {
             if (k0 == 0) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+            __syncwarp();
             tc_fence_after_sync();
-            const uint32_t tS = taddr + (uint32_t)g * (kt + d16);
-            for (int ks = 0; ks < d16 / 16; ++ks)
-              tc_mma_f16(tS, tile_desc_rows(aq + (qb * NWG + g) * qtile + ks * 256, d16),
-                         tile_desc_rows(ak + st * ktile + ks * 256, d16), idesc, ks > 0 ? 1u : 0u);
-            tc_commit(&s_full[g]);
+            if (elect_one()) {
+              mma_steps(taddr + (uint32_t)g * (kt + d16), dq0 + (qb * NWG + g) * uq, 16, dk0 + st * uk, 16, d16 / 16, idesc, false);
+              tc_commit(&s_full[g]);
+            }
           }
         }
-        if (have && !reuse) tc_commit(&v_empty[pst]);  // all of the step before is issued
-        if (k.cnt > kt) tc_commit(&k_empty[st]);
+        if (elect_one()) {
+          if (have && !reuse) tc_commit(&v_empty[pst]);  // all of the step before is issued
+          if (k.cnt > kt) tc_commit(&k_empty[st]);
+        }
         have = true;
         if (!reuse) {
           pit = it++;
@@ -438,7 +445,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         pfirst = k0 == 0;
         plast = k0 + kt >= k.cnt;
       }
-      tc_commit(&q_empty[qb]);
+      if (elect_one()) tc_commit(&q_empty[qb]);
       ++qi;
     }
 #pragma unroll

@@ -52,6 +52,16 @@ __device__ __forceinline__ uint64_t tile_desc_cols(uint32_t base, int d16) {  //
   return tc_smem_desc(base, (uint32_t)d16 * 16, 128);
 }
 
+// n K steps of an MMA from descriptors whose start addresses move by `da`, `db`
+// 16-byte units a step; one thread. With A in TMEM a step is eight columns.
+__device__ __forceinline__ void mma_steps(uint32_t d, uint64_t a, uint32_t da, uint64_t b, uint32_t db, int n, uint32_t idesc,
+                                          bool add) {
+  for (int k = 0; k < n; ++k, a += da, b += db) tc_mma_f16(d, a, b, idesc, add || k > 0 ? 1u : 0u);
+}
+__device__ __forceinline__ void mma_steps_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t db, int n, uint32_t idesc, bool add) {
+  for (int k = 0; k < n; ++k, a += 8, b += db) tc_mma_f16_ta(d, a, b, idesc, add || k > 0 ? 1u : 0u);
+}
+
 // Bounded wait (about a second); after a failure a thread no longer waits, runs
 // on with accesses in bounds, and the call's results are not valid.
 __device__ __forceinline__ void wait_or_bad(uint64_t* bar, uint32_t parity, bool& bad, int32_t* status) {

@@ -135,6 +135,19 @@ __device__ __forceinline__ void tmem_st(uint32_t t, const uint32_t (&r)[16]) {
       : "memory");
 }
 
+// Whole warp: true in one lane, the same one each time. A loop of MMAs runs in
+// whole warps with this around what one thread issues, so that addresses and
+// descriptors stay in uniform registers: an MMA issued from a branch of a single
+// lane took 200 cycles of moving its operands there.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+// A value that all lanes of a warp agree on, in a form the compiler knows that of.
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 // Instruction descriptor for kind::f16 with fp32 accumulators: operands both
 // float16 (bf16 = 0) or both bfloat16 (1); at, bt: A, B lie with their M, N axis
 // contiguous (in place of K).
