@@ -22,7 +22,7 @@ namespace pa {
 namespace {
 
 constexpr int kSms = 152;
-constexpr size_t kSmemMost = 222 << 10;
+constexpr size_t kSmemMost = 220 << 10;
 
 // Sources' items in order, by source: a CTA per source.
 constexpr int kOrderThreads = 256;
@@ -70,22 +70,31 @@ struct DqShape {
   int kt, d16, stages, qbufs, tiles, groups, su;
   uint32_t tmem;
 };
-constexpr int kTable = 256;
+constexpr int kTable = 128;  // work items of a CTA that are looked up at the start
 
-constexpr int kLoadThreads = 7 * 32;  // with the warp that issues the MMAs a multiple of four warps
+struct __align__(16) Work {
+  int g, cnt, n, j, group, pad[3];  // source, its keys that count; item; key head; group of tiles
+};
+
+// A warp per group issues its MMAs; loader warps fill up to a multiple of four
+// (registers are given out by four warps).
+template <int NWG>
+__host__ __device__ constexpr int dq_load() {
+  return (8 - NWG) * 32;
+}
 template <int NWG>
 __host__ __device__ constexpr int dq_threads() {
-  return NWG * 128 + kLoadThreads + 32;
+  return NWG * 160 + dq_load<NWG>();
 }
 
 // stat: [item][key head][row of the key head] (lse log2 e, delta) for k_attn_dkv
 template <typename T, int NWG>
 __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Keys keys, DqShape sh, float2* __restrict__ stat) {
-  constexpr int kBf16 = Elem<T>::kBf16;
+  constexpr int kBf16 = Elem<T>::kBf16, LT = dq_load<NWG>();
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[2], k_empty[2], s_full[NWG], p_full[NWG], o_full[NWG];
   __shared__ uint32_t s_taddr;
-  __shared__ int2 s_work[kTable];
+  __shared__ Work s_work[kTable];
   __shared__ int64_t s_rows[2][128];
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
@@ -95,10 +104,10 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
   unsigned char* so = sk + sh.stages * 2 * ktile;
   if (tid == 0) {
     for (int b = 0; b < 2; ++b) {
-      for (int g = 0; g < NWG; ++g) mbar_init(&q_full[b][g], kLoadThreads);
-      mbar_init(&q_empty[b], 1);
-      mbar_init(&k_full[b], kLoadThreads);
-      mbar_init(&k_empty[b], 1);
+      for (int g = 0; g < NWG; ++g) mbar_init(&q_full[b][g], LT);
+      mbar_init(&q_empty[b], NWG);
+      mbar_init(&k_full[b], LT);
+      mbar_init(&k_empty[b], NWG);
     }
     for (int g = 0; g < NWG; ++g) {
       mbar_init(&s_full[g], 1);
@@ -124,12 +133,15 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
   pdl_wait();
   pdl_trigger();
   const int works = items_of(a.count, a.N) * sh.groups * a.J;
-  struct Work {
-    int n, j, group, g, cnt;
-  };
   auto look = [&](int w) {
-    const int g = source_of(a.src, a.src_stride, w / (a.J * sh.groups), a.G, a.status);
-    return make_int2(g, g < 0 ? 0 : keys.count(g));
+    Work k;
+    k.j = w % a.J;
+    w /= a.J;
+    k.group = w % sh.groups;
+    k.n = w / sh.groups;
+    k.g = source_of(a.src, a.src_stride, k.n, a.G, a.status);
+    k.cnt = k.g < 0 ? 0 : keys.count(k.g);
+    return k;
   };
   for (int i = tid; i < kTable; i += dq_threads<NWG>()) {
     const int64_t w = blockIdx.x + (int64_t)i * gridDim.x;
@@ -137,16 +149,8 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
   }
   __syncthreads();
   auto work = [&](int i, int w) {
-    Work k;
-    int2 f = i < kTable ? s_work[i] : look(w);
-    f.x = uniform(f.x);
-    f.y = uniform(f.y);
-    k.g = f.x;
-    k.cnt = f.y;
-    k.j = w % a.J;
-    w /= a.J;
-    k.group = w % sh.groups;
-    k.n = w / sh.groups;
+    Work k = i < kTable ? s_work[i] : look(w);
+    k.cnt = uniform(k.cnt);
     return k;
   };
   bool bad = false;
@@ -264,10 +268,10 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
       pending = true;
     }
     if (pending) finish(pend, false);
-  } else if (warp < 4 * NWG + kLoadThreads / 32) {
+  } else if (warp < 4 * NWG + LT / 32) {
     // ================= loads =================
     const int lt = tid - 4 * NWG * 32;
-    RowTables<kLoadThreads> tab{s_rows, 0};
+    RowTables<LT> tab{s_rows, 0};
     uint32_t it = 0, qi = 0;
     int hg = -1, hj = 0;  // the keys that stay
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
@@ -286,8 +290,8 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
             if (it >= (uint32_t)sh.stages) wait_or_bad(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
             const int n = min(kt, k.cnt - k0);
             const uint32_t to = smem_u32(sk + st * 2 * ktile);
-            copy_keys<kLoadThreads, T>(tab, to, kp, a.ks.token, keys, k.g, k0, n, (n + 15) & ~15, D, d16, lt);
-            copy_keys<kLoadThreads, T>(tab, to + ktile, vp, a.vs.token, keys, k.g, k0, n, (n + 15) & ~15, D, d16, lt);
+            copy_keys<LT, T>(tab, to, kp, a.ks.token, keys, k.g, k0, n, (n + 15) & ~15, D, d16, lt);
+            copy_keys<LT, T>(tab, to + ktile, vp, a.vs.token, keys, k.g, k0, n, (n + 15) & ~15, D, d16, lt);
             copies_arrive(&k_full[st]);
             ++it;
           }
@@ -301,8 +305,8 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
               if (tile < sh.tiles) {
                 const uint32_t m0 = (uint32_t)tile * 128;
                 const uint32_t to = smem_u32(sq + (qb * NWG + g) * 2 * qtile);
-                copy_queries<kLoadThreads, T>(tab, to, qp, a.qs, m0, R, a.Q, D, d16, lt);
-                copy_queries<kLoadThreads, T>(tab, to + qtile, dp, a.dos, m0, R, a.Q, D, d16, lt);
+                copy_queries<LT, T>(tab, to, qp, a.qs, m0, R, a.Q, D, d16, lt);
+                copy_queries<LT, T>(tab, to + qtile, dp, a.dos, m0, R, a.Q, D, d16, lt);
               }
               copies_arrive(&q_full[qb][g]);
             }
@@ -313,25 +317,23 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
     }
     copies_drain();
   } else {
-    // ================= MMAs =================
-    const uint64_t dq0 = tile_desc_rows(smem_u32(sq), d16), dk0 = tile_desc_rows(smem_u32(sk), d16),
+    // ================= MMAs of one group =================
+    const int g = uniform(warp - 4 * NWG - LT / 32);
+    const uint64_t dq0 = tile_desc_rows(smem_u32(sq) + g * 2 * qtile, d16), dk0 = tile_desc_rows(smem_u32(sk), d16),
                    dc0 = tile_desc_cols(smem_u32(sk), d16);
-    const uint32_t uq = qtile / 16, uk = ktile / 16, idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
+    const uint32_t uq = qtile / 16, uk = ktile / 16, tS = taddr + (uint32_t)g * cols;
+    const uint32_t idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
     uint32_t it = 0, qi = 0, p_par = 0;
     int hg = -1, hj = 0;
-    bool pv[NWG], plast = false, pfirst = false, pmul = false, have = false;
-#pragma unroll
-    for (int g = 0; g < NWG; ++g) pv[g] = false;
+    bool pv = false, plast = false, pfirst = false, pmul = false, have = false;  // the step before
     uint32_t pst = 0;
     int pn16 = 0;
-    auto second = [&](int g) {  // the step before is taken; dQ += dS K in the second sweep
-      wait_or_bad(&p_full[g], (p_par >> g) & 1u, bad, a.status);
-      p_par ^= 1u << g;
+    auto second = [&]() {  // the step before is taken; dQ += dS K in the second sweep
+      wait_or_bad(&p_full[g], p_par, bad, a.status);
+      p_par ^= 1;
       __syncwarp();
       tc_fence_after_sync();
-      if (!pmul) return;
-      const uint32_t tS = taddr + (uint32_t)g * cols;
-      if (elect_one()) {
+      if (pmul && elect_one()) {
         mma_steps_ta(tS + 2 * kt, tS, dc0 + pst * 2 * uk, d16 * 2, pn16 / 16, idesc2, !pfirst);
         if (plast) tc_commit(&o_full[g]);
       }
@@ -339,63 +341,57 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
       const Work k = work(i, w);
       if (k.cnt <= 0) continue;
-      const bool one = k.cnt <= kt, reuse = hg == k.g && hj == k.j;
+      const bool one = k.cnt <= kt, reuse = hg == k.g && hj == k.j, valid = k.group * NWG + g < sh.tiles;
       hg = one ? k.g : -1;
       hj = k.j;
       const uint32_t qb = qi % sh.qbufs;
       for (int sweep = one ? 1 : 0; sweep < 2; ++sweep) {
         for (int k0 = 0; k0 < k.cnt; k0 += kt) {
           const int n16 = (min(kt, k.cnt - k0) + 15) & ~15;
+          const bool begin = k0 == 0 && sweep == (one ? 1 : 0), end = sweep == 1 && k0 + kt >= k.cnt;
           uint32_t st = pst;
           if (!reuse) {
             st = it % sh.stages;
-            // one stage: it has to be given back before it can be filled again
-            if (sh.stages == 1 && have) {
-#pragma unroll
-              for (int g = 0; g < NWG; ++g)
-                if (pv[g]) {
-                  second(g);
-                  pv[g] = false;
-                }
+            if (sh.stages == 1 && have) {  // it has to be given back before it can be filled again
+              if (pv) second();
+              pv = false;
+              __syncwarp();
               if (elect_one()) tc_commit(&k_empty[pst]);
             }
             landed(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
           }
-          const uint32_t idesc = tc_idesc_16(128, n16, kBf16, 0, 0);
-          const bool firsts = k0 == 0 && sweep == (one ? 1 : 0);
-#pragma unroll
-          for (int g = 0; g < NWG; ++g) {
-            if (pv[g]) second(g);
-            pv[g] = k.group * NWG + g < sh.tiles;
-            if (pv[g]) {
-              if (firsts) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
-              __syncwarp();
-              tc_fence_after_sync();
-              if (elect_one()) {
-                const uint32_t tS = taddr + (uint32_t)g * cols;
-                const uint64_t q = dq0 + (qb * NWG + g) * 2 * uq, kk = dk0 + st * 2 * uk;
-                mma_steps(tS, q, 16, kk, 16, d16 / 16, idesc, false);
-                mma_steps(tS + kt, q + uq, 16, kk + uk, 16, d16 / 16, idesc, false);
-                tc_commit(&s_full[g]);
-              }
+          if (pv) second();
+          pv = valid;
+          // without a tile it waits all the same: it must not run ahead of the loaders
+          if (begin) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+          if (valid) {
+            __syncwarp();
+            tc_fence_after_sync();
+            if (elect_one()) {
+              const uint32_t idesc = tc_idesc_16(128, n16, kBf16, 0, 0);
+              const uint64_t q = dq0 + qb * NWG * 2 * uq, kk = dk0 + st * 2 * uk;
+              mma_steps(tS, q, 16, kk, 16, d16 / 16, idesc, false);
+              mma_steps(tS + kt, q + uq, 16, kk + uk, 16, d16 / 16, idesc, false);
+              tc_commit(&s_full[g]);
             }
           }
-          if (have && !reuse && sh.stages > 1 && elect_one()) tc_commit(&k_empty[pst]);
+          __syncwarp();
+          if (elect_one()) {
+            if (have && !reuse && sh.stages > 1) tc_commit(&k_empty[pst]);
+            if (end) tc_commit(&q_empty[qb]);
+          }
           have = true;
           if (!reuse) ++it;
           pst = st;
           pn16 = n16;
           pmul = sweep == 1;
           pfirst = k0 == 0;
-          plast = sweep == 1 && k0 + kt >= k.cnt;
+          plast = end;
         }
       }
-      if (elect_one()) tc_commit(&q_empty[qb]);
       ++qi;
     }
-#pragma unroll
-    for (int g = 0; g < NWG; ++g)
-      if (pv[g]) second(g);
+    if (pv) second();
   }
   __syncthreads();
   __syncwarp();
@@ -409,7 +405,8 @@ struct DkvShape {
   uint32_t tmem;
 };
 constexpr int kDkvStages = 4;
-constexpr int kDkvThreads = 2 * 128 + kLoadThreads + 32;
+constexpr int kLoadThreads = 6 * 32;
+constexpr int kDkvThreads = 2 * 128 + kLoadThreads + 2 * 32;
 constexpr int kKeyTile = 128;
 
 // part: [part][dv, dk][source][key head][key in the list][D]
@@ -419,7 +416,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
                const int32_t* __restrict__ order, float* __restrict__ part) {
   constexpr int kBf16 = Elem<T>::kBf16;
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ __align__(8) uint64_t q_full[kDkvStages], q_empty[kDkvStages], k_full, s_full[2], p_full[2], done;
+  __shared__ __align__(8) uint64_t q_full[kDkvStages], q_empty[kDkvStages], k_full, s_full[2], p_full[2], s_free[2], done;
   __shared__ uint32_t s_taddr;
   __shared__ __align__(16) float2 s_stat[kDkvStages][64];
   __shared__ int64_t s_off[2][2][64], s_rows[2][128];
@@ -457,6 +454,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
     for (int s = 0; s < 2; ++s) {
       mbar_init(&s_full[s], 1);
       mbar_init(&p_full[s], 4);
+      mbar_init(&s_free[s], 1);
     }
     mbar_init(&done, 1);
     fence_barrier_init();
@@ -574,17 +572,16 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
       copies_arrive(&q_full[st]);
     }
     copies_drain();
-  } else if (tiles > 0) {
-    // ================= MMAs =================
+  } else if (warp == 8 + kLoadThreads / 32) {
+    // ================= MMAs: S^T and dP^T, two tiles ahead =================
     const uint64_t dk0 = tile_desc_rows(smem_u32(sk), d16), dv0 = tile_desc_rows(smem_u32(sv), d16),
-                   dq0 = tile_desc_rows(smem_u32(sq), d16), dc0 = tile_desc_cols(smem_u32(sq), d16);
-    const uint32_t uq = qtile / 16, uc = d16 * 2;
-    const uint32_t idesc = tc_idesc_16(128, qt, kBf16, 0, 0), idesc2 = tc_idesc_16(128, dn, kBf16, 0, 1);
-    uint32_t p_par = 0;
-    landed(&k_full, 0, bad, a.status);
-    auto scores = [&](int i) {
+                   dq0 = tile_desc_rows(smem_u32(sq), d16);
+    const uint32_t uq = qtile / 16, idesc = tc_idesc_16(128, qt, kBf16, 0, 0);
+    if (tiles > 0) landed(&k_full, 0, bad, a.status);
+    for (int i = 0; i < tiles; ++i) {
       const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt;
       landed(&q_full[st], (i / sh.stages) & 1u, bad, a.status);
+      if (i >= 2) wait_or_bad(&s_free[s], (i / 2 - 1) & 1u, bad, a.status);
       __syncwarp();
       tc_fence_after_sync();
       if (elect_one()) {
@@ -592,24 +589,25 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
         mma_steps(tS + qt, dv0, 16, dq0 + (st * 2 + 1) * uq, 16, d16 / 16, idesc, false);
         tc_commit(&s_full[s]);
       }
-    };
-    scores(0);
-    if (tiles > 1) scores(1);
+    }
+  } else {
+    // ================= MMAs: dV += P^T dO, dK += dS^T Q =================
+    const uint64_t dc0 = tile_desc_cols(smem_u32(sq), d16) + c0;  // c0 columns: c0 / 8 core matrices of 128 bytes
+    const uint32_t uq = qtile / 16, uc = d16 * 2, idesc = tc_idesc_16(128, dn, kBf16, 0, 1);
     for (int i = 0; i < tiles; ++i) {
       const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt;
-      wait_or_bad(&p_full[s], (p_par >> s) & 1u, bad, a.status);
-      p_par ^= 1u << s;
+      landed(&q_full[st], (i / sh.stages) & 1u, bad, a.status);
+      wait_or_bad(&p_full[s], (i / 2) & 1u, bad, a.status);
       __syncwarp();
       tc_fence_after_sync();
       if (elect_one()) {
-        const uint64_t q = dc0 + st * 2 * uq + c0;  // c0 columns: c0 / 8 core matrices of 128 bytes
-        mma_steps_ta(acc, tS, q + uq, uc, qt / 16, idesc2, i > 0);
-        mma_steps_ta(acc + dn, tS + qt, q, uc, qt / 16, idesc2, i > 0);
+        mma_steps_ta(acc, tS, dc0 + (st * 2 + 1) * uq, uc, qt / 16, idesc, i > 0);
+        mma_steps_ta(acc + dn, tS + qt, dc0 + st * 2 * uq, uc, qt / 16, idesc, i > 0);
         tc_commit(&q_empty[st]);
+        tc_commit(&s_free[s]);
+        if (i == tiles - 1) tc_commit(&done);
       }
-      if (i + 2 < tiles) scores(i + 2);
     }
-    if (elect_one()) tc_commit(&done);
   }
   __syncthreads();
   __syncwarp();
@@ -710,7 +708,7 @@ Plan plan(const AttnArgs& a) {
   if (v.qt > 64) v.qt = 64;
   v.stages = kDkvStages;
   const auto kv_smem = [&] { return (2 * (size_t)kKeyTile + (size_t)v.stages * 2 * v.qt) * d16 * 2; };
-  while (kv_smem() > kSmemMost - 4096) {
+  while (kv_smem() > kSmemMost - 2048) {
     if (v.stages > 2) --v.stages;
     else v.qt -= 16;
   }

@@ -6,9 +6,9 @@
 //   S = Q K^T        (both operands in shared memory, S in TMEM)
 //   P = exp2(c S - c m), c = scale log2 e, m the running maximum of the row
 //   O += P V         (P written over S in TMEM as the A operand, V as it lies)
-// One thread issues the MMAs of all groups in turn, so while one group's MMAs run
-// the others do their exponentials; a group hands P over and goes on to the next
-// S. O stays in TMEM; it is rescaled only where a row's maximum grows by more than
+// Each group has a warp that issues its MMAs (one for all of them was the bound: about
+// 100 cycles of issue and waits per MMA); while a group waits for its MMAs the others do
+// their exponentials. O stays in TMEM; it is rescaled only where a row's maximum grows by more than
 // 2^8 (probabilities stay below 2^8, which both 16-bit types hold). The last O of a
 // work item is read only after the next one's P is written, so no group waits for
 // its MMAs there.
@@ -26,7 +26,11 @@
 namespace pa {
 namespace {
 
-constexpr int kTable = 256;  // work items of a CTA whose source and keys are looked up at the start
+constexpr int kTable = 128;  // work items of a CTA that are looked up at the start
+
+struct __align__(16) Work {
+  int g, lo, cnt, n, j, group, part, pad;  // source; keys lo .. lo + cnt - 1; item; key head; group of tiles; part
+};
 
 struct TcShape {
   int kt, d16, stages, qbufs, splits;
@@ -36,16 +40,15 @@ struct TcShape {
 
 __host__ __device__ inline int stage_units(int D) { return D / 8 < 8 ? D / 8 : 8; }  // 16-byte units of a staged row
 
-// Loader warps: with the warp that issues the MMAs a multiple of four (registers
-// are given out by four warps). Two groups go over many key tiles, whose copies
-// are most of the loaders' work.
+// A warp per group issues its MMAs; loader warps fill up to a multiple of four
+// (registers are given out by four warps).
 template <int NWG>
 __host__ __device__ constexpr int tc_load() {
-  return (NWG <= 2 ? 7 : 3) * 32;
+  return (NWG == 4 ? 4 : 8 - NWG) * 32;
 }
 template <int NWG>
 __host__ __device__ constexpr int tc_threads() {
-  return NWG * 128 + tc_load<NWG>() + 32;
+  return NWG * 160 + tc_load<NWG>();
 }
 
 template <typename T, int NWG>
@@ -56,7 +59,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[NWG],
       p_full[NWG], o_full[NWG];
   __shared__ uint32_t s_taddr;
-  __shared__ int2 s_work[kTable];
+  __shared__ Work s_work[kTable];
   __shared__ int64_t s_rows[2][128];
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
@@ -68,11 +71,11 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   if (tid == 0) {
     for (int b = 0; b < 2; ++b) {
       for (int g = 0; g < NWG; ++g) mbar_init(&q_full[b][g], LT);
-      mbar_init(&q_empty[b], 1);
+      mbar_init(&q_empty[b], NWG);
       mbar_init(&k_full[b], LT);
-      mbar_init(&k_empty[b], 1);
+      mbar_init(&k_empty[b], NWG);
       mbar_init(&v_full[b], LT);
-      mbar_init(&v_empty[b], 1);
+      mbar_init(&v_empty[b], NWG);
     }
     for (int g = 0; g < NWG; ++g) {
       mbar_init(&s_full[g], 1);
@@ -99,14 +102,25 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   pdl_trigger();
   const int works = items_of(a.count, a.N) * sh.groups * a.J * sh.splits;
 
-  // ---- work items: item n, key head j, group of tiles, part of the keys
-  struct Work {
-    int n, j, group, part, g, lo, cnt;
-  };
-  auto look = [&](int w) {  // source and number of keys that count
-    const int n = w / (sh.splits * a.J * sh.groups);
-    const int g = source_of(a.src, a.src_stride, n, a.G, a.status);
-    return make_int2(g, g < 0 ? 0 : keys.count(g));
+  // ---- work items: item n, key head j, group of tiles, part of the keys; the
+  // first ones of a CTA are looked up by all threads at once
+  auto look = [&](int w) {
+    Work k;
+    k.part = sh.splits > 1 ? w % sh.splits : 0;
+    w /= sh.splits;
+    k.j = w % a.J;
+    w /= a.J;
+    k.group = w % sh.groups;
+    k.n = w / sh.groups;
+    k.g = source_of(a.src, a.src_stride, k.n, a.G, a.status);
+    k.lo = 0;
+    k.cnt = k.g < 0 ? 0 : keys.count(k.g);
+    if (sh.splits > 1) {
+      const int tiles = (k.cnt + kt - 1) / kt, t0 = tiles * k.part / sh.splits, t1 = tiles * (k.part + 1) / sh.splits;
+      k.lo = t0 * kt;
+      k.cnt = min(k.cnt, t1 * kt) - k.lo;
+    }
+    return k;
   };
   for (int i = tid; i < kTable; i += tc_threads<NWG>()) {
     const int64_t w = blockIdx.x + (int64_t)i * gridDim.x;
@@ -114,25 +128,8 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   }
   __syncthreads();
   auto work = [&](int i, int w) {
-    Work k;
-    int2 f = i < kTable ? s_work[i] : look(w);
-    f.x = uniform(f.x);
-    f.y = uniform(f.y);
-    k.g = f.x;
-    k.part = sh.splits > 1 ? w % sh.splits : 0;
-    w /= sh.splits;
-    k.j = w % a.J;
-    w /= a.J;
-    k.group = w % sh.groups;
-    k.n = w / sh.groups;
-    if (sh.splits > 1) {
-      const int tiles = (f.y + kt - 1) / kt, t0 = tiles * k.part / sh.splits, t1 = tiles * (k.part + 1) / sh.splits;
-      k.lo = t0 * kt;
-      k.cnt = min(f.y, t1 * kt) - k.lo;
-    } else {
-      k.lo = 0;
-      k.cnt = f.y;
-    }
+    Work k = i < kTable ? s_work[i] : look(w);
+    k.cnt = uniform(k.cnt);
     return k;
   };
   bool bad = false;
@@ -371,28 +368,27 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
     }
     copies_drain();
   } else {
-    // ================= MMAs =================
-    const uint64_t dq0 = tile_desc_rows(smem_u32(sq), d16), dk0 = tile_desc_rows(smem_u32(sk), d16),
+    // ================= MMAs of one group =================
+    const int g = uniform(warp - 4 * NWG - LT / 32);
+    const uint64_t dq0 = tile_desc_rows(smem_u32(sq) + g * qtile, d16), dk0 = tile_desc_rows(smem_u32(sk), d16),
                    dv0 = tile_desc_cols(smem_u32(sv), d16);
-    const uint32_t uq = qtile / 16, uk = ktile / 16, idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
-    uint32_t it = 0, qi = 0, p_par = 0;  // p_par: a bit per group
+    const uint32_t uq = NWG * qtile / 16, uk = ktile / 16, tS = taddr + (uint32_t)g * (kt + d16);
+    const uint32_t idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
+    uint32_t it = 0, qi = 0, p_par = 0;
     int hg = -1, hj = 0, hlo = 0, hcnt = 0;
-    // the step whose O += P V are still to come
-    bool pv[NWG], v_ready = true, plast = false, pfirst = false, have = false;
-#pragma unroll
-    for (int g = 0; g < NWG; ++g) pv[g] = false;
+    // the step before: its O += P V is still to come (pv)
+    bool pv = false, v_ready = true, plast = false, pfirst = false, have = false;
     uint32_t pst = 0, pit = 0;
     int pn16 = 0;
-    auto second = [&](int g) {  // O += P V of the step before
-      wait_or_bad(&p_full[g], (p_par >> g) & 1u, bad, a.status);
-      p_par ^= 1u << g;
+    auto second = [&]() {
+      wait_or_bad(&p_full[g], p_par, bad, a.status);
+      p_par ^= 1;
       if (!v_ready) {
         landed(&v_full[pst], (pit / sh.stages) & 1u, bad, a.status);
         v_ready = true;
       }
       __syncwarp();
       tc_fence_after_sync();
-      const uint32_t tS = taddr + (uint32_t)g * (kt + d16);
       if (elect_one()) {
         mma_steps_ta(tS + kt, tS, dv0 + pst * uk, d16 * 2, pn16 / 16, idesc2, !pfirst);
         if (plast) tc_commit(&o_full[g]);
@@ -402,7 +398,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       const Work k = work(i, w);
       if (k.cnt <= 0) continue;
       const bool reuse = hg == k.g && hj == k.j && hlo == k.lo && hcnt == k.cnt;
-      const bool held = hg >= 0;
+      const bool held = hg >= 0, valid = k.group * NWG + g < sh.tiles;
       hg = k.cnt <= kt ? k.g : -1;
       hj = k.j;
       hlo = k.lo;
@@ -412,28 +408,28 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         const int n16 = (min(kt, k.cnt - k0) + 15) & ~15;
         uint32_t st = pst;
         if (!reuse) {
+          __syncwarp();
           if (k0 == 0 && held && elect_one()) tc_commit(&k_empty[pst]);  // the keys that stayed are used up
           st = it % sh.stages;
           landed(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
         }
-        const uint32_t idesc = tc_idesc_16(128, n16, kBf16, 0, 0);
-#pragma unroll
-        for (int g = 0; g < NWG; ++g) {
-          if (pv[g]) second(g);
-          pv[g] = k.group * NWG + g < sh.tiles;
-          if (pv[g]) {
-            if (k0 == 0) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
-            __syncwarp();
-            tc_fence_after_sync();
-            if (elect_one()) {
-              mma_steps(taddr + (uint32_t)g * (kt + d16), dq0 + (qb * NWG + g) * uq, 16, dk0 + st * uk, 16, d16 / 16, idesc, false);
-              tc_commit(&s_full[g]);
-            }
+        if (pv) second();
+        pv = valid;
+        // without a tile it waits all the same: it must not run ahead of the loaders
+        if (k0 == 0) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+        if (valid) {
+          __syncwarp();
+          tc_fence_after_sync();
+          if (elect_one()) {
+            mma_steps(tS, dq0 + qb * uq, 16, dk0 + st * uk, 16, d16 / 16, tc_idesc_16(128, n16, kBf16, 0, 0), false);
+            tc_commit(&s_full[g]);
           }
         }
+        __syncwarp();
         if (elect_one()) {
           if (have && !reuse) tc_commit(&v_empty[pst]);  // all of the step before is issued
           if (k.cnt > kt) tc_commit(&k_empty[st]);
+          if (k0 + kt >= k.cnt) tc_commit(&q_empty[qb]);
         }
         have = true;
         if (!reuse) {
@@ -445,12 +441,9 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         pfirst = k0 == 0;
         plast = k0 + kt >= k.cnt;
       }
-      if (elect_one()) tc_commit(&q_empty[qb]);
       ++qi;
     }
-#pragma unroll
-    for (int g = 0; g < NWG; ++g)
-      if (pv[g]) second(g);
+    if (pv) second();
   }
   __syncthreads();
   __syncwarp();
@@ -464,7 +457,7 @@ struct TcPlan {
   size_t smem;
 };
 constexpr int kSms = 152;
-constexpr size_t kSmemMost = 222 << 10;
+constexpr size_t kSmemMost = 220 << 10;
 
 size_t tc_smem(int nwg, const TcShape& sh, int D) {
   const size_t row = (size_t)sh.d16 * 2;
