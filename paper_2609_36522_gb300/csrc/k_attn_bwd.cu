@@ -87,7 +87,7 @@ __host__ __device__ constexpr int dq_threads() {
   return NWG * 160 + dq_load<NWG>();
 }
 
-// stat: [item][key head][row of the key head] (lse log2 e, delta) for k_attn_dkv
+// stat: [item][key head][row of the key head] (-lse log2 e, -delta) for k_attn_dkv
 template <typename T, int NWG>
 __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Keys keys, DqShape sh, float2* __restrict__ stat) {
   constexpr int kBf16 = Elem<T>::kBf16, LT = dq_load<NWG>();
@@ -173,34 +173,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
         __syncwarp();
         tc_fence_after_sync();
       }
-      const float scale = bad ? __int_as_float(0x7fffffff) : empty ? 0.f : a.scale;
-      for (int c0 = 0; c0 < D; c0 += su * 8) {
-        for (int c = c0; c < min(c0 + su * 8, D); c += 16) {
-          uint32_t r[16] = {};
-          if (!empty) {
-            tmem_ld(tO + c, r);
-            tmem_ld_wait();
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (h && c + 8 >= D) break;
-            float v[8];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(r[8 * h + q]) * scale;
-            *reinterpret_cast<uint4*>(stage + (lane * sstride + (c - c0) / 8 + h) * 16) = Elem<T>::pack(v);
-          }
-        }
-        __syncwarp();
-        const int units = min(su, (D - c0) / 8);
-        for (int q = 0; q < su; ++q) {
-          const uint32_t e = q * 32 + lane, r = (e * usu) >> 16, u = e - r * su;
-          const int64_t off = __shfl_sync(0xffffffffu, row, r);
-          if (off >= 0 && (int)u < units)
-            *reinterpret_cast<uint4*>((T*)a.dq + off + c0 + u * 8) =
-                *reinterpret_cast<const uint4*>(stage + (r * sstride + u) * 16);
-        }
-        __syncwarp();
-      }
+      rows_out<T>((T*)a.dq, row, tO, D, bad ? __int_as_float(0x7fffffff) : a.scale, empty, stage, su, sstride, usu, lane);
     };
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
       const Work k = work(i, w);
@@ -224,37 +197,46 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
           s_par ^= 1;
           __syncwarp();
           tc_fence_after_sync();
+          const F2 c22(c2, c2), nl2(-l2, -l2);
           if (sweep == 0 || one) {
-            float sum[4] = {};
-            for (int c = 0; c < n16; c += 16) {
-              uint32_t r[16], d[16];
-              tmem_ld(tS + c, r);
-              tmem_ld(tP + c, d);
-              tmem_ld_wait();
+            F2 sum(0.f, 0.f);
+            columns2<32>(tS, tP, n16, [&](auto& r, auto& d, int c) {
+              constexpr int N = sizeof(r) / 4;
+              if (c + N > n) {  // exp2 of -infinity: 0
 #pragma unroll
-              for (int q = 0; q < 16; ++q) {
-                const float p = c + q < n ? ex2(fmaf(__uint_as_float(r[q]), c2, -l2)) : 0.f;
-                sum[q & 3] = fmaf(p, __uint_as_float(d[q]), sum[q & 3]);
+                for (int q = 0; q < N; ++q) r[q] = c + q < n ? r[q] : 0xff800000u;
               }
-            }
-            delta += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+              for (int q = 0; q < N; q += 2) {
+                float x, y;
+                fma2(F2(r[q], r[q + 1]), c22, nl2).get(x, y);
+                x = ex2(x);
+                y = ex2(y);
+                sum = fma2(F2(x, y), F2(d[q], d[q + 1]), sum);
+              }
+            });
+            float x, y;
+            sum.get(x, y);
+            delta += x + y;
           }
           if (sweep == 1) {
-            for (int c = 0; c < n16; c += 16) {
-              uint32_t r[16], d[16], s[8];
-              tmem_ld(tS + c, r);
-              tmem_ld(tP + c, d);
-              tmem_ld_wait();
+            const F2 nd(-delta, -delta);
+            columns2<32>(tS, tP, n16, [&](auto& r, auto& d, int c) {
+              constexpr int N = sizeof(r) / 4;
+              uint32_t s[N / 2];
+              if (c + N > n) {
 #pragma unroll
-              for (int q = 0; q < 16; q += 2) {
-                float x = ex2(fmaf(__uint_as_float(r[q]), c2, -l2)) * (__uint_as_float(d[q]) - delta);
-                float y = ex2(fmaf(__uint_as_float(r[q + 1]), c2, -l2)) * (__uint_as_float(d[q + 1]) - delta);
-                x = c + q < n ? x : 0.f;
-                y = c + q + 1 < n ? y : 0.f;
+                for (int q = 0; q < N; ++q) r[q] = c + q < n ? r[q] : 0xff800000u;
+              }
+#pragma unroll
+              for (int q = 0; q < N; q += 2) {
+                float x, y;
+                fma2(F2(r[q], r[q + 1]), c22, nl2).get(x, y);
+                mul2(F2(ex2(x), ex2(y)), add2(F2(d[q], d[q + 1]), nd)).get(x, y);
                 s[q / 2] = Elem<T>::pack2(x, y);
               }
               tmem_st(tS + c / 2, s);
-            }
+            });
             if (k0 == 0 && pending) finish(pend, false);
             tmem_st_wait();
           }
@@ -263,7 +245,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
           if (lane == 0) mbar_arrive(&p_full[g]);
         }
       }
-      if (there) stat[((int64_t)k.n * a.J + k.j) * a.Q * R + m] = make_float2(l2, delta);
+      if (there) stat[((int64_t)k.n * a.J + k.j) * a.Q * R + m] = make_float2(-l2, -delta);
       pend = row;
       pending = true;
     }
@@ -418,7 +400,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ __align__(8) uint64_t q_full[kDkvStages], q_empty[kDkvStages], k_full, s_full[2], p_full[2], s_free[2], done;
   __shared__ uint32_t s_taddr;
-  __shared__ __align__(16) float2 s_stat[kDkvStages][64];
+  __shared__ __align__(16) float s_stat[kDkvStages][128];  // per two rows: both -lse log2 e, both -delta
   __shared__ int64_t s_off[2][2][64], s_rows[2][128];
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, qt = sh.qt, rows_item = a.Q * R;
@@ -489,21 +471,24 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
       __syncwarp();
       tc_fence_after_sync();
       const float4* st = reinterpret_cast<const float4*>(s_stat[i % sh.stages]);
-      for (int c = 0; c < qt; c += 16) {
-        uint32_t r[16], d[16], pp[8], ds[8];
-        tmem_ld(tS + c, r);
-        tmem_ld(tP + c, d);
-        tmem_ld_wait();
+      const F2 c22(c2, c2);
+      columns2<32>(tS, tP, qt, [&](auto& r, auto& d, int c) {
+        constexpr int N = sizeof(r) / 4;
+        uint32_t pp[N / 2], ds[N / 2];
 #pragma unroll
-        for (int q = 0; q < 16; q += 2) {
-          const float4 f = st[(c + q) / 2];  // lse, delta of two rows
-          const float x = ex2(fmaf(__uint_as_float(r[q]), c2, -f.x)), y = ex2(fmaf(__uint_as_float(r[q + 1]), c2, -f.z));
+        for (int q = 0; q < N; q += 2) {
+          const float4 f = st[(c + q) / 2];  // -lse, -delta of two rows
+          float x, y, u, v;
+          fma2(F2(r[q], r[q + 1]), c22, F2(f.x, f.y)).get(x, y);
+          x = ex2(x);
+          y = ex2(y);
           pp[q / 2] = Elem<T>::pack2(x, y);
-          ds[q / 2] = Elem<T>::pack2(x * (__uint_as_float(d[q]) - f.y), y * (__uint_as_float(d[q + 1]) - f.w));
+          mul2(F2(x, y), add2(F2(d[q], d[q + 1]), F2(f.z, f.w))).get(u, v);
+          ds[q / 2] = Elem<T>::pack2(u, v);
         }
         tmem_st(tS + c / 2, pp);
         tmem_st(tP + c / 2, ds);
-      }
+      });
       tmem_st_wait();
       tc_fence_before_sync();
       __syncwarp();
@@ -561,9 +546,12 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
         }
         s_off[i & 1][0][lt] = oq;
         s_off[i & 1][1][lt] = od;
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(&s_stat[st][lt])), "l"(f),
-                     "r"(oq >= 0 ? 8 : 0)
-                     : "memory");
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(
+                           smem_u32(&s_stat[st][(lt >> 1) * 4 + w * 2 + (lt & 1)])),
+                       "l"(reinterpret_cast<const float*>(f) + w), "r"(oq >= 0 ? 4 : 0)
+                       : "memory");
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kLoadThreads) : "memory");
       const uint32_t to = smem_u32(sq + st * 2 * qtile);

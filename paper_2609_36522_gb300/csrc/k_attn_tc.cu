@@ -8,14 +8,19 @@
 //   O += P V         (P written over S in TMEM as the A operand, V as it lies)
 // Each group has a warp that issues its MMAs (one for all of them was the bound: about
 // 100 cycles of issue and waits per MMA); while a group waits for its MMAs the others do
-// their exponentials. O stays in TMEM; it is rescaled only where a row's maximum grows by more than
-// 2^8 (probabilities stay below 2^8, which both 16-bit types hold). The last O of a
-// work item is read only after the next one's P is written, so no group waits for
-// its MMAs there.
+// their exponentials. O stays in TMEM; it is rescaled only where a row's maximum grows
+// by more than 2^8 (probabilities stay below 2^8, which both 16-bit types hold). The
+// last O of a work item is read only after the next one's P is written, so no group
+// waits for its MMAs there.
+//
+// Two forms, by the number of keys. Up to 128 keys are one tile, S has one place
+// (L = 1) and as many groups as TMEM holds share an SM: the work per row is short and what
+// counts is rows in flight. More keys are taken 64 at a time with two places for S (L =
+// 2), so that the next S is there when a group comes for it.
 //
 // The loader warps copy Q, K and V with 16-byte asynchronous copies, ahead of use;
-// keys are picked from the list of those that count. Where all keys are one tile and the next
-// work item has the same ones (rows of one trajectory), K and V stay in shared
+// keys are picked from the list of those that count. Where all keys are one tile and the
+// next work item has the same ones (rows of one trajectory), K and V stay in shared
 // memory: CTAs take work items in turn, heads innermost, so that a CTA keeps its
 // head while neighbouring CTAs read the other heads of the same tokens.
 //
@@ -26,7 +31,8 @@
 namespace pa {
 namespace {
 
-constexpr int kTable = 128;  // work items of a CTA that are looked up at the start
+constexpr int kTable = 128;   // work items of a CTA that are looked up at the start
+constexpr int kStages = 4;    // of keys and values, at most
 
 struct __align__(16) Work {
   int g, lo, cnt, n, j, group, part, pad;  // source; keys lo .. lo + cnt - 1; item; key head; group of tiles; part
@@ -40,8 +46,7 @@ struct TcShape {
 
 __host__ __device__ inline int stage_units(int D) { return D / 8 < 8 ? D / 8 : 8; }  // 16-byte units of a staged row
 
-// A warp per group issues its MMAs; loader warps fill up to a multiple of four
-// (registers are given out by four warps).
+// Loader warps fill up to a multiple of four warps (registers are given out by four).
 template <int NWG>
 __host__ __device__ constexpr int tc_load() {
   return (NWG == 4 ? 4 : 8 - NWG) * 32;
@@ -51,19 +56,19 @@ __host__ __device__ constexpr int tc_threads() {
   return NWG * 160 + tc_load<NWG>();
 }
 
-template <typename T, int NWG>
+template <typename T, int NWG, int L>
 __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
     k_attn_tc(AttnArgs a, Keys keys, TcShape sh, float* __restrict__ po, float* __restrict__ pl) {
   constexpr int kBf16 = Elem<T>::kBf16, LT = tc_load<NWG>();
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[NWG],
-      p_full[NWG], o_full[NWG];
+  __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[kStages], k_empty[kStages], v_full[kStages],
+      v_empty[kStages], s_full[NWG][L], p_full[NWG][L], o_full[NWG];
   __shared__ uint32_t s_taddr;
   __shared__ Work s_work[kTable];
   __shared__ int64_t s_rows[2][128];
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
-  const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2;
+  const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2, cols = L * kt + d16;
   unsigned char* sq = smem;
   unsigned char* sk = sq + sh.qbufs * NWG * qtile;
   unsigned char* sv = sk + sh.stages * ktile;
@@ -72,14 +77,18 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
     for (int b = 0; b < 2; ++b) {
       for (int g = 0; g < NWG; ++g) mbar_init(&q_full[b][g], LT);
       mbar_init(&q_empty[b], NWG);
+    }
+    for (int b = 0; b < kStages; ++b) {
       mbar_init(&k_full[b], LT);
       mbar_init(&k_empty[b], NWG);
       mbar_init(&v_full[b], LT);
       mbar_init(&v_empty[b], NWG);
     }
     for (int g = 0; g < NWG; ++g) {
-      mbar_init(&s_full[g], 1);
-      mbar_init(&p_full[g], 4);
+      for (int b = 0; b < L; ++b) {
+        mbar_init(&s_full[g][b], 1);
+        mbar_init(&p_full[g][b], 4);
+      }
       mbar_init(&o_full[g], 1);
     }
     fence_barrier_init();
@@ -137,77 +146,47 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   if (warp < 4 * NWG) {
     // ================= softmax: a thread per row =================
     const int g = warp >> 2;
-    const uint32_t tS = taddr + (uint32_t)g * (kt + d16) + ((uint32_t)(warp & 3) << 21), tO = tS + kt;
+    const uint32_t t0 = taddr + (uint32_t)g * cols + ((uint32_t)(warp & 3) << 21), tO = t0 + L * kt;
     const float c2 = a.scale * kLog2e;
     const int su = stage_units(D), sstride = su | 1;
     const uint32_t usu = 65536u / su + 1;
     unsigned char* stage = so + warp * 32 * sstride * 16;
-    uint32_t s_par = 0, o_par = 0;
-    struct Pending {
+    uint32_t sc = 0;  // key tiles of this group so far
+    struct Pending {  // a work item whose O is to be written
       int64_t off, row;  // this thread's row: in out (elements), among all rows; negative: none
       int part;
       float m, l;
-      bool any;
     } pend;
-    pend.any = false;
+    bool pending = false;
+    auto mmas_done = [&](uint32_t c) {  // the O += P V of this group's first c key tiles
+      wait_or_bad(&o_full[g], (c - 1) & 1u, bad, a.status);
+      __syncwarp();
+      tc_fence_after_sync();
+    };
     // O / l of a work item to out
-    auto finish = [&](const Pending& f, bool empty) {
-      const float inv = empty ? 0.f : 1.f / f.l;
+    auto finish = [&](const Pending& f, bool empty, uint32_t c) {
+      float scale = 0.f, l2 = -INFINITY;
       if (!empty) {
-        wait_or_bad(&o_full[g], o_par, bad, a.status);
-        o_par ^= 1;
-        __syncwarp();
-        tc_fence_after_sync();
+        mmas_done(c);
+        scale = bad ? __int_as_float(0x7fffffff) : 1.f / f.l;
+        l2 = f.m * c2 + log2f(f.l);
       }
-      const float scale = bad ? __int_as_float(0x7fffffff) : inv;
       if (sh.splits > 1) {
         float* o = po + (f.row * sh.splits + f.part) * D;
-        for (int c = 0; c < d16; c += 16) {
-          uint32_t r[16] = {};
-          if (!empty) {
-            tmem_ld(tO + c, r);
-            tmem_ld_wait();
-          }
-          if (f.row >= 0) {
+        columns<16>(tO, d16, [&](auto& r, int c) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-              if (c + 4 * q < D)
-                *reinterpret_cast<float4*>(o + c + 4 * q) =
-                    make_float4(__uint_as_float(r[4 * q]) * scale, __uint_as_float(r[4 * q + 1]) * scale,
-                                __uint_as_float(r[4 * q + 2]) * scale, __uint_as_float(r[4 * q + 3]) * scale);
-          }
-        }
-        if (f.row >= 0) pl[f.row * sh.splits + f.part] = empty ? -INFINITY : f.m * c2 + log2f(f.l);
+          for (int q = 0; q < 4; ++q)
+            if (f.row >= 0 && c + 4 * q < D)
+              *reinterpret_cast<float4*>(o + c + 4 * q) =
+                  empty ? make_float4(0.f, 0.f, 0.f, 0.f)
+                        : make_float4(__uint_as_float(r[4 * q]) * scale, __uint_as_float(r[4 * q + 1]) * scale,
+                                      __uint_as_float(r[4 * q + 2]) * scale, __uint_as_float(r[4 * q + 3]) * scale);
+        });
+        if (f.row >= 0) pl[f.row * sh.splits + f.part] = l2;
         return;
       }
-      if (f.row >= 0 && a.lse) a.lse[f.row] = empty ? -INFINITY : (f.m * c2 + log2f(f.l)) * kLn2;
-      for (int c0 = 0; c0 < D; c0 += su * 8) {
-        for (int c = c0; c < min(c0 + su * 8, D); c += 16) {
-          uint32_t r[16] = {};
-          if (!empty) {
-            tmem_ld(tO + c, r);
-            tmem_ld_wait();
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (h && c + 8 >= D) break;
-            float v[8];
-#pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(r[8 * h + q]) * scale;
-            *reinterpret_cast<uint4*>(stage + (lane * sstride + (c - c0) / 8 + h) * 16) = Elem<T>::pack(v);
-          }
-        }
-        __syncwarp();
-        const int units = min(su, (D - c0) / 8);  // the rows' pieces, neighbouring lanes on neighbouring pieces
-        for (int q = 0; q < su; ++q) {
-          const uint32_t e = q * 32 + lane, row = (e * usu) >> 16, u = e - row * su;
-          const int64_t off = __shfl_sync(0xffffffffu, f.off, row);
-          if (off >= 0 && (int)u < units)
-            *reinterpret_cast<uint4*>((T*)a.o + off + c0 + u * 8) =
-                *reinterpret_cast<const uint4*>(stage + (row * sstride + u) * 16);
-        }
-        __syncwarp();
-      }
+      if (f.row >= 0 && a.lse) a.lse[f.row] = l2 * kLn2;
+      rows_out<T>((T*)a.o, f.off, tO, D, scale, empty, stage, su, sstride, usu, lane);
     };
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
       const Work k = work(i, w);
@@ -221,103 +200,114 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         cur.off = there ? k.n * a.os.item + t * a.os.token + h * a.os.head : -1;
         cur.row = there ? ((int64_t)k.n * a.Q + t) * a.H + h : -1;
         cur.part = k.part;
-        cur.any = true;
       }
       if (k.cnt <= 0) {
-        finish(cur, true);
+        finish(cur, true, 0);
         continue;
       }
       cur.m = -INFINITY;
       cur.l = 0.f;
-      for (int k0 = 0; k0 < k.cnt; k0 += kt) {
+      const uint32_t before = sc;
+      for (int k0 = 0; k0 < k.cnt; k0 += kt, ++sc) {
         const int n = min(kt, k.cnt - k0), n16 = (n + 15) & ~15;
-        wait_or_bad(&s_full[g], s_par, bad, a.status);
-        s_par ^= 1;
+        const uint32_t b = L == 1 ? 0 : sc & 1u, tS = t0 + b * kt;
+        wait_or_bad(&s_full[g][b], (sc / L) & 1u, bad, a.status);
         __syncwarp();
         tc_fence_after_sync();
-        // the tile's maximum
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        int c = 0;
-        for (; c + 32 <= n16; c += 32) {
-          uint32_t r[32];
-          tmem_ld(tS + c, r);
-          tmem_ld_wait();
-          if (c + 32 <= n) {
-#pragma unroll
-            for (int q = 0; q < 32; ++q) mx[q & 3] = fmaxf(mx[q & 3], __uint_as_float(r[q]));
+        // a new maximum of the row: O and the sum are scaled where it grows by much
+        auto raise = [&](float m) {
+          if (k0 == 0) {
+            cur.m = m;
           } else {
+            const bool grow = (m - cur.m) * c2 > 8.f;
+            if (__any_sync(0xffffffffu, grow)) {
+              mmas_done(sc);
+              const float f = grow ? ex2((cur.m - m) * c2) : 1.f;
+              if (grow) cur.m = m;
+              cur.l *= f;
+#pragma unroll 1
+              for (int o = 0; o < d16; o += 16) {
+                uint32_t r[16];
+                tmem_ld(tO + o, r);
+                tmem_ld_wait();
 #pragma unroll
-            for (int q = 0; q < 32; ++q) mx[q & 3] = fmaxf(mx[q & 3], c + q < n ? __uint_as_float(r[q]) : -INFINITY);
-          }
-        }
-        if (c < n16) {
-          uint32_t r[16];
-          tmem_ld(tS + c, r);
-          tmem_ld_wait();
-#pragma unroll
-          for (int q = 0; q < 16; ++q) mx[q & 3] = fmaxf(mx[q & 3], c + q < n ? __uint_as_float(r[q]) : -INFINITY);
-        }
-        const float m = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        if (k0 == 0) {
-          cur.m = m;
-        } else {
-          const bool grow = (m - cur.m) * c2 > 8.f;
-          if (__any_sync(0xffffffffu, grow)) {  // the MMAs before this S are complete: O may be changed
-            const float f = grow ? ex2((cur.m - m) * c2) : 1.f;
-            if (grow) cur.m = m;
-            cur.l *= f;
-            for (int o = 0; o < d16; o += 16) {
-              uint32_t r[16];
-              tmem_ld(tO + o, r);
-              tmem_ld_wait();
-#pragma unroll
-              for (int q = 0; q < 16; ++q) r[q] = __float_as_uint(__uint_as_float(r[q]) * f);
-              tmem_st(tO + o, r);
+                for (int q = 0; q < 16; ++q) r[q] = __float_as_uint(__uint_as_float(r[q]) * f);
+                tmem_st(tO + o, r);
+              }
             }
           }
-        }
-        const float mc = cur.m == -INFINITY ? 0.f : cur.m * c2;
-        float sum[4] = {};
-        auto probs = [&](auto& r, auto& p, int c, bool whole) {
-          constexpr int W = sizeof(r) / 4;
-#pragma unroll
-          for (int q = 0; q < W; q += 2) {
-            float x = ex2(fmaf(__uint_as_float(r[q]), c2, -mc)), y = ex2(fmaf(__uint_as_float(r[q + 1]), c2, -mc));
-            if (!whole) {
-              x = c + q < n ? x : 0.f;
-              y = c + q + 1 < n ? y : 0.f;
-            }
-            sum[q & 2] += x;
-            sum[(q & 2) + 1] += y;
-            p[q / 2] = Elem<T>::pack2(x, y);
-          }
+          return cur.m == -INFINITY ? 0.f : -cur.m * c2;
         };
-        c = 0;
-        for (; c + 32 <= n16; c += 32) {
-          uint32_t r[32], p[16];
-          tmem_ld(tS + c, r);
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if constexpr (L == 2) {
+          uint32_t r[64], p[32];  // the row's values stay here
+          tmem_ld(tS, r);
           tmem_ld_wait();
-          if (c + 32 <= n) probs(r, p, c, true);
-          else probs(r, p, c, false);
-          tmem_st(tS + c / 2, p);
+          if (n < 64) {
+#pragma unroll
+            for (int q = 0; q < 64; ++q) r[q] = q < n ? r[q] : 0xff800000u;
+          }
+#pragma unroll
+          for (int q = 0; q < 64; q += 2) mx[q / 2 & 3] = max3(mx[q / 2 & 3], __uint_as_float(r[q]), __uint_as_float(r[q + 1]));
+          const float mc = raise(max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]));
+          const F2 c22(c2, c2), mc2(mc, mc);
+          F2 sum[2] = {F2(0.f, 0.f), F2(0.f, 0.f)};
+#pragma unroll
+          for (int q = 0; q < 32; ++q) {
+            float x, y;
+            fma2(F2(r[2 * q], r[2 * q + 1]), c22, mc2).get(x, y);
+            x = ex2(x);
+            y = ex2(y);
+            sum[q & 1] = add2(sum[q & 1], F2(x, y));
+            p[q] = Elem<T>::pack2(x, y);
+          }
+          tmem_st(tS, p);
+          float x, y;
+          add2(sum[0], sum[1]).get(x, y);
+          cur.l += x + y;
+        } else {
+          columns<32>(tS, n16, [&](auto& r, int c) {
+            constexpr int N = sizeof(r) / 4;
+            if (c + N <= n) {
+#pragma unroll
+              for (int q = 0; q < N; q += 2)
+                mx[q / 2 & 3] = max3(mx[q / 2 & 3], __uint_as_float(r[q]), __uint_as_float(r[q + 1]));
+            } else {
+#pragma unroll
+              for (int q = 0; q < N; ++q) mx[q & 3] = fmaxf(mx[q & 3], c + q < n ? __uint_as_float(r[q]) : -INFINITY);
+            }
+          });
+          const float mc = raise(max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]));
+          float sum[4] = {};
+          columns<32>(tS, n16, [&](auto& r, int c) {
+            constexpr int N = sizeof(r) / 4;
+            uint32_t p[N / 2];
+            const bool whole = c + N <= n;
+#pragma unroll
+            for (int q = 0; q < N; q += 2) {
+              float x = ex2(fmaf(__uint_as_float(r[q]), c2, mc)), y = ex2(fmaf(__uint_as_float(r[q + 1]), c2, mc));
+              if (!whole) {
+                x = c + q < n ? x : 0.f;
+                y = c + q + 1 < n ? y : 0.f;
+              }
+              sum[q & 2] += x;
+              sum[(q & 2) + 1] += y;
+              p[q / 2] = Elem<T>::pack2(x, y);
+            }
+            tmem_st(tS + c / 2, p);
+          });
+          cur.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         }
-        if (c < n16) {
-          uint32_t r[16], p[8];
-          tmem_ld(tS + c, r);
-          tmem_ld_wait();
-          probs(r, p, c, false);
-          tmem_st(tS + c / 2, p);
-        }
-        cur.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        if (k0 == 0 && pend.any) finish(pend, false);
+        if (k0 == 0 && pending) finish(pend, false, before);
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[g]);
+        if (lane == 0) mbar_arrive(&p_full[g][b]);
       }
       pend = cur;
+      pending = true;
     }
-    if (pend.any) finish(pend, false);
+    if (pending) finish(pend, false, sc);
   } else if (warp < 4 * NWG + LT / 32) {
     // ================= loads =================
     const int lt = tid - 4 * NWG * 32;
@@ -372,26 +362,35 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
     const int g = uniform(warp - 4 * NWG - LT / 32);
     const uint64_t dq0 = tile_desc_rows(smem_u32(sq) + g * qtile, d16), dk0 = tile_desc_rows(smem_u32(sk), d16),
                    dv0 = tile_desc_cols(smem_u32(sv), d16);
-    const uint32_t uq = NWG * qtile / 16, uk = ktile / 16, tS = taddr + (uint32_t)g * (kt + d16);
+    const uint32_t uq = NWG * qtile / 16, uk = ktile / 16, t0 = taddr + (uint32_t)g * cols;
     const uint32_t idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
-    uint32_t it = 0, qi = 0, p_par = 0;
+    uint32_t it = 0, qi = 0, sc = 0, v_seen = 0;  // key tiles loaded, work items, key tiles of this group, tiles of V waited for
     int hg = -1, hj = 0, hlo = 0, hcnt = 0;
-    // the step before: its O += P V is still to come (pv)
-    bool pv = false, v_ready = true, plast = false, pfirst = false, have = false;
-    uint32_t pst = 0, pit = 0;
-    int pn16 = 0;
-    auto second = [&]() {
-      wait_or_bad(&p_full[g], p_par, bad, a.status);
-      p_par ^= 1;
-      if (!v_ready) {
-        landed(&v_full[pst], (pit / sh.stages) & 1u, bad, a.status);
-        v_ready = true;
-      }
-      __syncwarp();
-      tc_fence_after_sync();
-      if (elect_one()) {
-        mma_steps_ta(tS + kt, tS, dv0 + pst * uk, d16 * 2, pn16 / 16, idesc2, !pfirst);
-        if (plast) tc_commit(&o_full[g]);
+    struct Step {  // a key tile whose S is issued and whose O += P V is not
+      uint32_t st, it, sc;
+      int n16;
+      bool valid, first, release;  // this group has a tile; overwrites O; V is not used after it
+    };
+    Step older, newer;  // (older: L = 2 only)
+    int waiting = 0;
+    auto second = [&](const Step& e) {
+      if (e.valid) {
+        const uint32_t b = L == 1 ? 0 : e.sc & 1u;
+        wait_or_bad(&p_full[g][b], (e.sc / L) & 1u, bad, a.status);
+        if (e.it >= v_seen) {
+          landed(&v_full[e.st], (e.it / sh.stages) & 1u, bad, a.status);
+          v_seen = e.it + 1;
+        }
+        __syncwarp();
+        tc_fence_after_sync();
+        if (elect_one()) {
+          mma_steps_ta(t0 + L * kt, t0 + b * kt, dv0 + e.st * uk, d16 * 2, e.n16 / 16, idesc2, !e.first);
+          tc_commit(&o_full[g]);
+          if (e.release) tc_commit(&v_empty[e.st]);
+        }
+      } else {
+        __syncwarp();
+        if (e.release && elect_one()) tc_commit(&v_empty[e.st]);
       }
     };
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
@@ -405,45 +404,54 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       hcnt = k.cnt;
       const uint32_t qb = qi % sh.qbufs;
       for (int k0 = 0; k0 < k.cnt; k0 += kt) {
-        const int n16 = (min(kt, k.cnt - k0) + 15) & ~15;
-        uint32_t st = pst;
-        if (!reuse) {
+        Step s;
+        s.n16 = (min(kt, k.cnt - k0) + 15) & ~15;
+        s.valid = valid;
+        s.first = k0 == 0;
+        s.release = true;
+        if (waiting) newer.release = !reuse;
+        if (reuse) {
+          s.st = newer.st;
+          s.it = newer.it;
+        } else {
           __syncwarp();
-          if (k0 == 0 && held && elect_one()) tc_commit(&k_empty[pst]);  // the keys that stayed are used up
-          st = it % sh.stages;
-          landed(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
+          if (k0 == 0 && held && elect_one()) tc_commit(&k_empty[newer.st]);  // the keys that stayed are used up
+          if (L == 1 && sh.stages == 1 && waiting) {  // the only stage: it has to be given back first
+            second(newer);
+            waiting = 0;
+          }
+          s.it = it++;
+          s.st = s.it % sh.stages;
+          landed(&k_full[s.st], (s.it / sh.stages) & 1u, bad, a.status);
         }
-        if (pv) second();
-        pv = valid;
+        if (waiting == L) {
+          second(L == 1 ? newer : older);
+          --waiting;
+        }
         // without a tile it waits all the same: it must not run ahead of the loaders
         if (k0 == 0) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
-        if (valid) {
-          __syncwarp();
-          tc_fence_after_sync();
-          if (elect_one()) {
-            mma_steps(tS, dq0 + qb * uq, 16, dk0 + st * uk, 16, d16 / 16, tc_idesc_16(128, n16, kBf16, 0, 0), false);
-            tc_commit(&s_full[g]);
-          }
-        }
+        s.sc = sc;
         __syncwarp();
+        tc_fence_after_sync();
         if (elect_one()) {
-          if (have && !reuse) tc_commit(&v_empty[pst]);  // all of the step before is issued
-          if (k.cnt > kt) tc_commit(&k_empty[st]);
+          if (valid) {
+            const uint32_t b = L == 1 ? 0 : sc & 1u;
+            mma_steps(t0 + b * kt, dq0 + qb * uq, 16, dk0 + s.st * uk, 16, d16 / 16, tc_idesc_16(128, s.n16, kBf16, 0, 0),
+                      false);
+            tc_commit(&s_full[g][b]);
+          }
+          if (k.cnt > kt) tc_commit(&k_empty[s.st]);
           if (k0 + kt >= k.cnt) tc_commit(&q_empty[qb]);
         }
-        have = true;
-        if (!reuse) {
-          pit = it++;
-          v_ready = false;
-        }
-        pst = st;
-        pn16 = n16;
-        pfirst = k0 == 0;
-        plast = k0 + kt >= k.cnt;
+        if (valid) ++sc;
+        older = newer;
+        newer = s;
+        ++waiting;
       }
       ++qi;
     }
-    if (pv) second();
+    if (waiting == 2) second(older);
+    if (waiting) second(newer);
   }
   __syncthreads();
   __syncwarp();
@@ -453,6 +461,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
 // ---- shapes -------------------------------------------------------------------
 struct TcPlan {
   int nwg, grid;
+  bool two;  // two places for S
   TcShape sh;
   size_t smem;
 };
@@ -472,25 +481,25 @@ TcPlan tc_plan(const AttnArgs& a) {
   const int64_t rows = (int64_t)a.Q * (a.H / a.J);
   s.tiles = (int)((rows + 127) / 128);
   const int k16 = (a.K + 15) & ~15;
-  s.kt = k16 < 128 ? (k16 > 0 ? k16 : 16) : 128;
-  if (s.kt + s.d16 > 256 && s.d16 < 256) {  // two groups need narrower key tiles
-    const int kt = (256 - s.d16) & ~15;
-    if (kt >= 64) s.kt = kt;
-  }
-  p.nwg = 512 / (s.kt + s.d16);
-  if (p.nwg > 4) p.nwg = 4;
+  p.two = k16 > 128;
+  s.kt = p.two ? 64 : k16 > 0 ? k16 : 16;
+  p.nwg = 512 / ((p.two ? 2 : 1) * s.kt + s.d16);
+  const int most = p.two ? 2 : 4;
+  if (p.nwg > most) p.nwg = most;
   if (p.nwg > s.tiles) p.nwg = s.tiles;
+  if (p.nwg < 1) p.nwg = 1;
   s.qbufs = 2;
-  s.stages = 2;
+  s.stages = p.two ? kStages : 2;
+  // short of shared memory: one buffer of Q, then fewer groups, fewer stages
   while (tc_smem(p.nwg, s, a.D) > kSmemMost) {
     if (s.qbufs == 2) s.qbufs = 1;
-    else if (s.kt > 64) s.kt -= 16;
+    else if (s.stages > 2) --s.stages;
     else if (p.nwg > 1) --p.nwg;
     else s.stages = 1;
   }
   s.groups = (s.tiles + p.nwg - 1) / p.nwg;
   s.tmem = 32;
-  while (s.tmem < (uint32_t)(p.nwg * (s.kt + s.d16))) s.tmem <<= 1;
+  while (s.tmem < (uint32_t)(p.nwg * ((p.two ? 2 : 1) * s.kt + s.d16))) s.tmem <<= 1;
   // too few work items for the SMs: the keys are split, joined afterwards
   const int64_t works = (int64_t)a.N * s.groups * a.J, ktiles = (a.K + s.kt - 1) / s.kt;
   s.splits = 1;
@@ -505,12 +514,23 @@ TcPlan tc_plan(const AttnArgs& a) {
   return p;
 }
 
-template <typename T, int NWG>
+template <typename T, int NWG, int L>
 cudaError_t go(const AttnArgs& a, const Keys& keys, const TcPlan& p, float* po, float* pl, cudaStream_t st) {
   static SmemGranted granted;
-  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_tc<T, NWG>), p.smem, granted);
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_tc<T, NWG, L>), p.smem, granted);
   if (e != cudaSuccess) return e;
-  return launch_ex(k_attn_tc<T, NWG>, dim3(p.grid), dim3(tc_threads<NWG>()), p.smem, st, 0, a, keys, p.sh, po, pl);
+  return launch_ex(k_attn_tc<T, NWG, L>, dim3(p.grid), dim3(tc_threads<NWG>()), p.smem, st, 0, a, keys, p.sh, po, pl);
+}
+
+template <typename T>
+cudaError_t launch(const AttnArgs& a, const Keys& keys, const TcPlan& p, float* po, float* pl, cudaStream_t st) {
+  if (p.two) return p.nwg == 1 ? go<T, 1, 2>(a, keys, p, po, pl, st) : go<T, 2, 2>(a, keys, p, po, pl, st);
+  switch (p.nwg) {
+    case 1: return go<T, 1, 1>(a, keys, p, po, pl, st);
+    case 2: return go<T, 2, 1>(a, keys, p, po, pl, st);
+    case 3: return go<T, 3, 1>(a, keys, p, po, pl, st);
+    default: return go<T, 4, 1>(a, keys, p, po, pl, st);
+  }
 }
 
 }  // namespace
@@ -519,13 +539,7 @@ int attn_tc_splits(const AttnArgs& a) { return tc_plan(a).sh.splits; }
 
 cudaError_t launch_attn_tc(const AttnArgs& a, const Keys& keys, float* po, float* pl, cudaStream_t st) {
   const TcPlan p = tc_plan(a);
-  const bool half = a.dtype == 1;
-  switch (p.nwg) {
-    case 1: return half ? go<__half, 1>(a, keys, p, po, pl, st) : go<__nv_bfloat16, 1>(a, keys, p, po, pl, st);
-    case 2: return half ? go<__half, 2>(a, keys, p, po, pl, st) : go<__nv_bfloat16, 2>(a, keys, p, po, pl, st);
-    case 3: return half ? go<__half, 3>(a, keys, p, po, pl, st) : go<__nv_bfloat16, 3>(a, keys, p, po, pl, st);
-    default: return half ? go<__half, 4>(a, keys, p, po, pl, st) : go<__nv_bfloat16, 4>(a, keys, p, po, pl, st);
-  }
+  return a.dtype == 1 ? launch<__half>(a, keys, p, po, pl, st) : launch<__nv_bfloat16>(a, keys, p, po, pl, st);
 }
 
 }  // namespace pa

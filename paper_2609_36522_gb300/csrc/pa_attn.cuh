@@ -40,6 +40,104 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
+// Two fp32 values in one instruction.
+struct F2 {
+  uint64_t v;
+  __device__ __forceinline__ F2() {}
+  __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ F2(uint32_t a, uint32_t b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b)); }
+  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// f(values, first column) over the n16 TMEM columns (a multiple of 16) of this
+// thread's lane, W at a time, then 16. A load takes its latency whatever its width,
+// so few wide ones: 16 at a time with the next 16 on their way were slower (100 x 4096
+// tokens, 77 keys of 40: 214 us against 177).
+template <int N, typename F>
+__device__ __forceinline__ void column_block(uint32_t t, int c, F& f) {
+  uint32_t r[N];
+  tmem_ld(t + c, r);
+  tmem_ld_wait();
+  f(r, c);
+}
+template <int W, typename F>
+__device__ __forceinline__ void columns(uint32_t t, int n16, F f) {
+  int c = 0;
+  for (; c + W <= n16; c += W) column_block<W>(t, c, f);
+  if constexpr (W > 16)
+    for (; c < n16; c += 16) column_block<16>(t, c, f);
+}
+// The same over two sets of columns.
+template <int N, typename F>
+__device__ __forceinline__ void column_block2(uint32_t t, uint32_t u, int c, F& f) {
+  uint32_t r[N], d[N];
+  tmem_ld(t + c, r);
+  tmem_ld(u + c, d);
+  tmem_ld_wait();
+  f(r, d, c);
+}
+template <int W, typename F>
+__device__ __forceinline__ void columns2(uint32_t t, uint32_t u, int n16, F f) {
+  int c = 0;
+  for (; c + W <= n16; c += W) column_block2<W>(t, u, c, f);
+  if constexpr (W > 16)
+    if (c < n16) column_block2<16>(t, u, c, f);
+}
+
+// A warp's 32 rows of a tile, `scale` times the D columns from t on, to memory in
+// 16 bits: staged in shared memory (su 16-byte units of a row at a time, sstride
+// units apart; usu = 65536 / su + 1), then neighbouring lanes write neighbouring
+// units. off: where this lane's row goes, in elements (negative: nowhere). zero: zeros.
+template <typename T>
+__device__ __forceinline__ void rows_out(T* to, int64_t off, uint32_t t, int D, float scale, bool zero, unsigned char* stage,
+                                         int su, int sstride, uint32_t usu, int lane) {
+  for (int c0 = 0; c0 < D; c0 += su * 8) {
+    const int cols = min(su * 8, D - c0);
+    unsigned char* mine = stage + lane * sstride * 16;
+    if (zero) {
+      for (int u = 0; u < cols / 8; ++u) *reinterpret_cast<uint4*>(mine + u * 16) = make_uint4(0, 0, 0, 0);
+    } else {
+      columns<16>(t + c0, (cols + 15) & ~15, [&](auto& r, int c) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(r[8 * h + q]) * scale;
+          if (h == 0 || c + 8 < cols) *reinterpret_cast<uint4*>(mine + (c / 8 + h) * 16) = Elem<T>::pack(v);
+        }
+      });
+    }
+    __syncwarp();
+    for (int q = 0; q < su; ++q) {
+      const uint32_t e = q * 32 + lane, r = (e * usu) >> 16, u = e - r * su;
+      const int64_t o = __shfl_sync(0xffffffffu, off, r);
+      if (o >= 0 && (int)u * 8 < cols)
+        *reinterpret_cast<uint4*>(to + o + c0 + u * 8) = *reinterpret_cast<const uint4*>(stage + (r * sstride + u) * 16);
+    }
+    __syncwarp();
+  }
+}
+
 // ---- tensor-core kernels: operand tiles and their copies ---------------------
 // A tile of rows [row][d] lies in shared memory as core matrices of 8 rows x 16
 // bytes, those of eight rows side by side: one layout in which the rows are M or
@@ -108,7 +206,7 @@ __device__ __forceinline__ void copy_rows(uint32_t dst, int rows, int valid, int
   const int dc = (LT / 8) % nch, dr = (LT / 8) / nch * 8;
   const int64_t dp = dr * stride + dc * 8, wp = 8 * stride - nch * 8;
   const uint32_t dd = (uint32_t)(dr >> 3) * d16 * 16 + dc * 128, wd = (uint32_t)d16 * 16 - nch * 128;
-#pragma unroll 4
+#pragma unroll 2
   while (row < rows) {
     copy16(dst, row < valid ? p : base, row < valid);
     c += dc;
@@ -133,7 +231,7 @@ __device__ __forceinline__ void copy_rows_at(uint32_t dst, int rows, int d, int 
   dst += (uint32_t)(row >> 3) * d16 * 16 + c * 128 + (row & 7) * 16;
   const int dc = (LT / 8) % nch, dr = (LT / 8) / nch * 8;
   const uint32_t dd = (uint32_t)(dr >> 3) * d16 * 16 + dc * 128, wd = (uint32_t)d16 * 16 - nch * 128;
-#pragma unroll 4
+#pragma unroll 2
   while (row < rows) {
     const int64_t o = off[row];
     copy16(dst, base + (o < 0 ? 0 : o + c * 8), o >= 0);
