@@ -314,6 +314,39 @@ cudaError_t launch_attn(const AttnArgs& a, cudaStream_t st) {
   return a.dtype == 1 ? run<__half>(a, st) : run<__nv_bfloat16>(a, st);
 }
 
+bool make_map(CUtensorMap* map, int dtype, const void* base, int D, int64_t n1, int64_t n2, int64_t n3, int64_t s1, int64_t s2,
+              int64_t s3, int cols, int b1, int b2, int sw) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess) {
+      (void)cudaGetLastError();
+      f = nullptr;
+    }
+    return reinterpret_cast<Encode>(f);
+  }();
+  if (!encode || n1 < 1 || n2 < 1 || n3 < 1 || b1 > 256 || b2 > 256 || cols > 256) return false;
+  // an axis of one entry has no stride that matters
+  const int64_t any = align_up((size_t)D * 2, 16);
+  const int64_t s[3] = {n1 > 1 ? s1 * 2 : any, n2 > 1 ? s2 * 2 : any, n3 > 1 ? s3 * 2 : any};
+  for (int64_t v : s)
+    if (v < 16 || v % 16 != 0 || v >= (int64_t)1 << 40) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)n1, (cuuint64_t)n2, (cuuint64_t)n3};
+  const cuuint64_t strides[3] = {(cuuint64_t)s[0], (cuuint64_t)s[1], (cuuint64_t)s[2]};
+  const cuuint32_t box[4] = {(cuuint32_t)cols, (cuuint32_t)b1, (cuuint32_t)b2, 1}, ones[4] = {1, 1, 1, 1};
+  const CUtensorMapSwizzle swizzle = sw == 128  ? CU_TENSOR_MAP_SWIZZLE_128B
+                                     : sw == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                     : sw == 32 ? CU_TENSOR_MAP_SWIZZLE_32B
+                                                : CU_TENSOR_MAP_SWIZZLE_NONE;
+  return encode(map, dtype == 1 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 cudaError_t attn_status(int32_t** out) {
   static std::atomic<int32_t*> known[64];
   int dev = 0;

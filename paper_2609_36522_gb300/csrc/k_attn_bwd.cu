@@ -67,6 +67,9 @@ __global__ void __launch_bounds__(kOrderThreads) k_attn_order(const int32_t* __r
 // ===========================================================================
 // dq
 struct DqShape {
+  Box box;
+  OutBox obox;
+  bool q_bulk, k_bulk, o_bulk;  // by tiled bulk copies
   int kt, d16, stages, qbufs, tiles, groups, su;
   uint32_t tmem;
 };
@@ -89,16 +92,18 @@ __host__ __device__ constexpr int dq_threads() {
 
 // stat: [item][key head][row of the key head] (-lse log2 e, -delta) for k_attn_dkv
 template <typename T, int NWG>
-__global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Keys keys, DqShape sh, float2* __restrict__ stat) {
+__global__ void __launch_bounds__(dq_threads<NWG>(), 1)
+    k_attn_dq(const __grid_constant__ Maps maps, AttnArgs a, Keys keys, DqShape sh, float2* __restrict__ stat) {
   constexpr int kBf16 = Elem<T>::kBf16, LT = dq_load<NWG>();
-  extern __shared__ __align__(128) unsigned char smem[];
+  extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[2], k_empty[2], s_full[NWG], p_full[NWG], o_full[NWG];
   __shared__ uint32_t s_taddr;
   __shared__ Work s_work[kTable];
   __shared__ int64_t s_rows[2][128];
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
-  const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2, cols = 2 * kt + d16;
+  const Box box = sh.box;
+  const uint32_t qtile = 128u * box.row_bytes(), ktile = (uint32_t)kt * box.row_bytes(), cols = 2 * kt + d16;
   unsigned char* sq = smem;                                 // per buffer and group: q, dout
   unsigned char* sk = sq + sh.qbufs * NWG * 2 * qtile;      // per stage: k, v
   unsigned char* so = sk + sh.stages * 2 * ktile;
@@ -116,11 +121,9 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
     }
     fence_barrier_init();
   }
-  if (D & 8) {  // the columns beyond D, once: no copy touches them
-    const int rows = sh.qbufs * NWG * 256 + 2 * sh.stages * kt;
-    for (int r = tid; r < rows; r += dq_threads<NWG>())
-      *reinterpret_cast<uint4*>(smem + (uint32_t)(r >> 3) * d16 * 16 + (d16 / 8 - 1) * 128 + (r & 7) * 16) =
-          make_uint4(0, 0, 0, 0);
+  if (D != box.row_bytes() / 2 && !(sh.q_bulk && sh.k_bulk && !a.len)) {  // the columns beyond D, once
+    const uint32_t bytes = 2 * sh.qbufs * NWG * qtile + 2 * sh.stages * ktile;
+    for (uint32_t o = tid * 16; o < bytes; o += dq_threads<NWG>() * 16) *reinterpret_cast<uint4*>(smem + o) = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
   }
   if (warp == 0) {
@@ -162,18 +165,25 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
     const float c2 = a.scale * kLog2e;
     const int su = sh.su, sstride = su | 1;
     const uint32_t usu = 65536u / su + 1;
-    unsigned char* stage = so + warp * 32 * sstride * 16;
+    unsigned char* stage = so + warp * (sh.o_bulk ? 32 * sh.obox.wide * 2 : 32 * sstride * 16);
     uint32_t s_par = 0, o_par = 0;
-    int64_t pend = -1;  // this thread's row of dq still to be written (elements; negative: none)
+    struct Pending {  // rows of dq to be written: this thread's place (elements, negative: none), or the first one's
+      int64_t off;
+      int n, head, token;
+    } pend;
     bool pending = false;
-    auto finish = [&](int64_t row, bool empty) {
+    auto finish = [&](const Pending& f, bool empty) {
       if (!empty) {
         wait_or_bad(&o_full[g], o_par, bad, a.status);
         o_par ^= 1;
         __syncwarp();
         tc_fence_after_sync();
       }
-      rows_out<T>((T*)a.dq, row, tO, D, bad ? __int_as_float(0x7fffffff) : a.scale, empty, stage, su, sstride, usu, lane);
+      const float scale = bad ? __int_as_float(0x7fffffff) : a.scale;
+      if (sh.o_bulk)
+        rows_out_bulk<T>(&maps.out, f.head, f.token, f.n, f.token < a.Q, tO, D, sh.obox, scale, empty, stage, lane);
+      else
+        rows_out<T>((T*)a.dq, f.off, tO, D, scale, empty, stage, su, sstride, usu, lane);
     };
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
       const Work k = work(i, w);
@@ -182,7 +192,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
       const uint32_t m = (uint32_t)tile * 128 + (warp & 3) * 32 + lane;
       const uint32_t t = R == 1 ? m : m / (uint32_t)R, h = k.j * R + (R == 1 ? 0 : m - t * R);
       const bool there = t < (uint32_t)a.Q;
-      const int64_t row = there ? k.n * a.dqs.item + t * a.dqs.token + h * a.dqs.head : -1;
+      const Pending row{there ? k.n * a.dqs.item + t * a.dqs.token + h * a.dqs.head : -1, k.n, k.j * R, uniform((int)t)};
       if (k.cnt <= 0) {
         finish(row, true);
         continue;
@@ -250,6 +260,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
       pending = true;
     }
     if (pending) finish(pend, false);
+    if (lane == 0) bulk_stores_done();
   } else if (warp < 4 * NWG + LT / 32) {
     // ================= loads =================
     const int lt = tid - 4 * NWG * 32;
@@ -272,9 +283,16 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
             if (it >= (uint32_t)sh.stages) wait_or_bad(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
             const int n = min(kt, k.cnt - k0);
             const uint32_t to = smem_u32(sk + st * 2 * ktile);
-            copy_keys<LT, T>(tab, to, kp, a.ks.token, keys, k.g, k0, n, (n + 15) & ~15, D, d16, lt);
-            copy_keys<LT, T>(tab, to + ktile, vp, a.vs.token, keys, k.g, k0, n, (n + 15) & ~15, D, d16, lt);
-            copies_arrive(&k_full[st]);
+            if (sh.k_bulk && (n == kt || !a.len)) {  // past a source's length lies anything: not by whole tiles
+              if (bulk_job(&k_full[st], 2 * ktile, lt)) {
+                bulk_tile(to, &maps.k, box, kt, k.j, k0, k.g, &k_full[st]);
+                bulk_tile(to + ktile, &maps.v, box, kt, k.j, k0, k.g, &k_full[st]);
+              }
+            } else {
+              copy_keys<LT, T>(tab, to, kp, a.ks.token, keys, k.g, k0, n, (n + 15) & ~15, kt, D, box, lt);
+              copy_keys<LT, T>(tab, to + ktile, vp, a.vs.token, keys, k.g, k0, n, (n + 15) & ~15, kt, D, box, lt);
+              copies_arrive(&k_full[st]);
+            }
             ++it;
           }
           if (k0 == 0 && sweep == (one ? 1 : 0)) {
@@ -284,11 +302,17 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
 #pragma unroll 1
             for (int g = 0; g < NWG; ++g) {
               const int tile = k.group * NWG + g;
+              const uint32_t to = smem_u32(sq + (qb * NWG + g) * 2 * qtile), m0 = (uint32_t)tile * 128;
+              if (tile < sh.tiles && sh.q_bulk) {
+                if (bulk_job(&q_full[qb][g], 2 * qtile, lt)) {
+                  bulk_tile(to, &maps.q, box, 128, k.j * R, m0 / R, k.n, &q_full[qb][g]);
+                  bulk_tile(to + qtile, &maps.dout, box, 128, k.j * R, m0 / R, k.n, &q_full[qb][g]);
+                }
+                continue;
+              }
               if (tile < sh.tiles) {
-                const uint32_t m0 = (uint32_t)tile * 128;
-                const uint32_t to = smem_u32(sq + (qb * NWG + g) * 2 * qtile);
-                copy_queries<LT, T>(tab, to, qp, a.qs, m0, R, a.Q, D, d16, lt);
-                copy_queries<LT, T>(tab, to + qtile, dp, a.dos, m0, R, a.Q, D, d16, lt);
+                copy_queries<LT, T>(tab, to, qp, a.qs, m0, R, a.Q, D, box, lt);
+                copy_queries<LT, T>(tab, to + qtile, dp, a.dos, m0, R, a.Q, D, box, lt);
               }
               copies_arrive(&q_full[qb][g]);
             }
@@ -301,8 +325,8 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
   } else {
     // ================= MMAs of one group =================
     const int g = uniform(warp - 4 * NWG - LT / 32);
-    const uint64_t dq0 = tile_desc_rows(smem_u32(sq) + g * 2 * qtile, d16), dk0 = tile_desc_rows(smem_u32(sk), d16),
-                   dc0 = tile_desc_cols(smem_u32(sk), d16);
+    const uint64_t dq0 = tile_desc_rows(smem_u32(sq) + g * 2 * qtile, box.sw), dk0 = tile_desc_rows(smem_u32(sk), box.sw),
+                   dc0 = tile_desc_cols(smem_u32(sk), box.sw, kt);
     const uint32_t uq = qtile / 16, uk = ktile / 16, tS = taddr + (uint32_t)g * cols;
     const uint32_t idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
     uint32_t it = 0, qi = 0, p_par = 0;
@@ -316,7 +340,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
       __syncwarp();
       tc_fence_after_sync();
       if (pmul && elect_one()) {
-        mma_steps_ta(tS + 2 * kt, tS, dc0 + pst * 2 * uk, d16 * 2, pn16 / 16, idesc2, !pfirst);
+        mma_over_rows(tS + 2 * kt, tS, dc0 + pst * 2 * uk, box.sw, pn16 / 16, idesc2, !pfirst);
         if (plast) tc_commit(&o_full[g]);
       }
     };
@@ -352,8 +376,8 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
             if (elect_one()) {
               const uint32_t idesc = tc_idesc_16(128, n16, kBf16, 0, 0);
               const uint64_t q = dq0 + qb * NWG * 2 * uq, kk = dk0 + st * 2 * uk;
-              mma_steps(tS, q, 16, kk, 16, d16 / 16, idesc, false);
-              mma_steps(tS + kt, q + uq, 16, kk + uk, 16, d16 / 16, idesc, false);
+              mma_over_d(tS, q, 128, kk, kt, box.sw, d16 / 16, idesc);
+              mma_over_d(tS + kt, q + uq, 128, kk + uk, kt, box.sw, d16 / 16, idesc);
               tc_commit(&s_full[g]);
             }
           }
@@ -383,6 +407,8 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1) k_attn_dq(AttnArgs a, Ke
 // ===========================================================================
 // dk and dv
 struct DkvShape {
+  Box box;
+  bool q_bulk, k_bulk;
   int qt, d16, stages, kb, parts, halves;  // rows of a tile; key tiles; parts of the rows; parts of the columns
   uint32_t tmem;
 };
@@ -391,13 +417,16 @@ constexpr int kLoadThreads = 6 * 32;
 constexpr int kDkvThreads = 2 * 128 + kLoadThreads + 2 * 32;
 constexpr int kKeyTile = 128;
 
+// Columns of dv and dk that a CTA adds up: all, or halves of whole blocks.
+__host__ __device__ inline int half_columns(int d16, int halves) { return halves == 1 ? d16 : (d16 / 2 + 63) / 64 * 64; }
+
 // part: [part][dv, dk][source][key head][key in the list][D]
 template <typename T>
 __global__ void __launch_bounds__(kDkvThreads, 1)
-    k_attn_dkv(AttnArgs a, Keys keys, DkvShape sh, const float2* __restrict__ stat, const int32_t* __restrict__ first,
+    k_attn_dkv(const __grid_constant__ Maps maps, AttnArgs a, Keys keys, DkvShape sh, const float2* __restrict__ stat, const int32_t* __restrict__ first,
                const int32_t* __restrict__ order, float* __restrict__ part) {
   constexpr int kBf16 = Elem<T>::kBf16;
-  extern __shared__ __align__(128) unsigned char smem[];
+  extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ __align__(8) uint64_t q_full[kDkvStages], q_empty[kDkvStages], k_full, s_full[2], p_full[2], s_free[2], done;
   __shared__ uint32_t s_taddr;
   __shared__ __align__(16) float s_stat[kDkvStages][128];  // per two rows: both -lse log2 e, both -delta
@@ -421,9 +450,9 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
   const int64_t t0 = all * p / sh.parts;
   const int tiles = (int)(all * (p + 1) / sh.parts - t0);
   // this CTA's columns of dv and dk
-  const int split16 = (d16 / 16 + sh.halves - 1) / sh.halves * 16;
-  const int c0 = half * split16, dn = min(split16, d16 - c0);
-  const uint32_t qtile = (uint32_t)qt * d16 * 2, ktile = (uint32_t)kKeyTile * d16 * 2;
+  const int c0 = half * half_columns(d16, sh.halves), dn = min(half_columns(d16, sh.halves), d16 - c0);
+  const Box box = sh.box;
+  const uint32_t qtile = (uint32_t)qt * box.row_bytes(), ktile = (uint32_t)kKeyTile * box.row_bytes();
   unsigned char* sk = smem;
   unsigned char* sv = sk + ktile;
   unsigned char* sq = sv + ktile;  // per stage: q, dout
@@ -441,11 +470,9 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
     mbar_init(&done, 1);
     fence_barrier_init();
   }
-  if (D & 8) {
-    const int n = 2 * kKeyTile + sh.stages * 2 * qt;
-    for (int r = tid; r < n; r += kDkvThreads)
-      *reinterpret_cast<uint4*>(smem + (uint32_t)(r >> 3) * d16 * 16 + (d16 / 8 - 1) * 128 + (r & 7) * 16) =
-          make_uint4(0, 0, 0, 0);
+  if (D != box.row_bytes() / 2 && !(sh.q_bulk && sh.k_bulk && !a.len)) {  // the columns beyond D, once
+    const uint32_t bytes = 2 * ktile + 2 * sh.stages * qtile;
+    for (uint32_t o = tid * 16; o < bytes; o += kDkvThreads * 16) *reinterpret_cast<uint4*>(smem + o) = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
   }
   if (warp == 0) {
@@ -525,13 +552,52 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
       const T* kp = (const T*)a.k + g * a.ks.item + j * a.ks.head;
       const T* vp = (const T*)a.v + g * a.vs.item + j * a.vs.head;
       const int n = min(kn, kKeyTile);
-      copy_keys<kLoadThreads, T>(tab, smem_u32(sk), kp, a.ks.token, keys, g, k0, n, kKeyTile, D, d16, lt);
-      copy_keys<kLoadThreads, T>(tab, smem_u32(sv), vp, a.vs.token, keys, g, k0, n, kKeyTile, D, d16, lt);
-      copies_arrive(&k_full);
+      if (sh.k_bulk && (n == kKeyTile || !a.len)) {  // past a source's length lies anything: not by whole tiles
+        if (bulk_job(&k_full, 2 * ktile, lt)) {
+          bulk_tile(smem_u32(sk), &maps.k, box, kKeyTile, j, k0, g, &k_full);
+          bulk_tile(smem_u32(sv), &maps.v, box, kKeyTile, j, k0, g, &k_full);
+        }
+      } else {
+        copy_keys<kLoadThreads, T>(tab, smem_u32(sk), kp, a.ks.token, keys, g, k0, n, kKeyTile, kKeyTile, D, box, lt);
+        copy_keys<kLoadThreads, T>(tab, smem_u32(sv), vp, a.vs.token, keys, g, k0, n, kKeyTile, kKeyTile, D, box, lt);
+        copies_arrive(&k_full);
+      }
+    }
+    int item = 0, within = 0, n = 0;  // by bulk copies a tile is of one item: which, and its first row there
+    if (sh.q_bulk && tiles > 0) {
+      item = (int)(t0 * qt / rows_item);
+      within = (int)(t0 * qt - (int64_t)item * rows_item);
+      n = order ? order[i0 + item] : i0 + item;
     }
     for (int i = 0; i < tiles; ++i) {
       const uint32_t st = i % sh.stages;
       if (i >= sh.stages) wait_or_bad(&q_empty[st], (i / sh.stages - 1) & 1u, bad, a.status);
+      auto stat_in = [&](const float* f, bool there) {  // row lt's -lse and -delta
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(
+                           smem_u32(&s_stat[st][(lt >> 1) * 4 + w * 2 + (lt & 1)])),
+                       "l"(f + w), "r"(there ? 4 : 0)
+                       : "memory");
+      };
+      const uint32_t to = smem_u32(sq + st * 2 * qtile);
+      if (sh.q_bulk) {
+        if (lt < qt) stat_in(reinterpret_cast<const float*>(stat + ((int64_t)n * a.J + j) * rows_item + within + lt), true);
+        if (lt == 0) {
+          fence_proxy_async_smem();
+          asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(&q_full[st])), "r"(2 * qtile)
+                       : "memory");
+          bulk_tile(to, &maps.q, box, qt, j * R, within / R, n, &q_full[st]);
+          bulk_tile(to + qtile, &maps.dout, box, qt, j * R, within / R, n, &q_full[st]);
+        }
+        copies_arrive(&q_full[st]);
+        if ((within += qt) == rows_item) {
+          within = 0;
+          ++item;
+          if (i + 1 < tiles) n = order ? order[i0 + item] : i0 + item;
+        }
+        continue;
+      }
       // where the rows lie
       if (lt < qt) {
         const int64_t m = (t0 + i) * qt + lt;
@@ -546,24 +612,21 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
         }
         s_off[i & 1][0][lt] = oq;
         s_off[i & 1][1][lt] = od;
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(
-                           smem_u32(&s_stat[st][(lt >> 1) * 4 + w * 2 + (lt & 1)])),
-                       "l"(reinterpret_cast<const float*>(f) + w), "r"(oq >= 0 ? 4 : 0)
-                       : "memory");
+        stat_in(reinterpret_cast<const float*>(f), oq >= 0);
       }
       asm volatile("bar.sync 1, %0;" ::"n"(kLoadThreads) : "memory");
-      const uint32_t to = smem_u32(sq + st * 2 * qtile);
-      copy_rows_at<kLoadThreads, T>(to, qt, D, d16, (const T*)a.q, s_off[i & 1][0], lt);
-      copy_rows_at<kLoadThreads, T>(to + qtile, qt, D, d16, (const T*)a.dout, s_off[i & 1][1], lt);
+      const int64_t* off = s_off[i & 1][0];
+      copy_rows<kLoadThreads, T>(to, qt, qt, D, box, (const T*)a.q, lt,
+                                 [&](int r) { return off[r] < 0 ? (const T*)nullptr : (const T*)a.q + off[r]; });
+      copy_rows<kLoadThreads, T>(to + qtile, qt, qt, D, box, (const T*)a.dout, lt,
+                                 [&](int r) { return off[64 + r] < 0 ? (const T*)nullptr : (const T*)a.dout + off[64 + r]; });
       copies_arrive(&q_full[st]);
     }
     copies_drain();
   } else if (warp == 8 + kLoadThreads / 32) {
     // ================= MMAs: S^T and dP^T, two tiles ahead =================
-    const uint64_t dk0 = tile_desc_rows(smem_u32(sk), d16), dv0 = tile_desc_rows(smem_u32(sv), d16),
-                   dq0 = tile_desc_rows(smem_u32(sq), d16);
+    const uint64_t dk0 = tile_desc_rows(smem_u32(sk), box.sw), dv0 = tile_desc_rows(smem_u32(sv), box.sw),
+                   dq0 = tile_desc_rows(smem_u32(sq), box.sw);
     const uint32_t uq = qtile / 16, idesc = tc_idesc_16(128, qt, kBf16, 0, 0);
     if (tiles > 0) landed(&k_full, 0, bad, a.status);
     for (int i = 0; i < tiles; ++i) {
@@ -573,15 +636,15 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
       __syncwarp();
       tc_fence_after_sync();
       if (elect_one()) {
-        mma_steps(tS, dk0, 16, dq0 + st * 2 * uq, 16, d16 / 16, idesc, false);
-        mma_steps(tS + qt, dv0, 16, dq0 + (st * 2 + 1) * uq, 16, d16 / 16, idesc, false);
+        mma_over_d(tS, dk0, kKeyTile, dq0 + st * 2 * uq, qt, box.sw, d16 / 16, idesc);
+        mma_over_d(tS + qt, dv0, kKeyTile, dq0 + (st * 2 + 1) * uq, qt, box.sw, d16 / 16, idesc);
         tc_commit(&s_full[s]);
       }
     }
   } else {
     // ================= MMAs: dV += P^T dO, dK += dS^T Q =================
-    const uint64_t dc0 = tile_desc_cols(smem_u32(sq), d16) + c0;  // c0 columns: c0 / 8 core matrices of 128 bytes
-    const uint32_t uq = qtile / 16, uc = d16 * 2, idesc = tc_idesc_16(128, dn, kBf16, 0, 1);
+    const uint64_t dc0 = tile_desc_cols(smem_u32(sq), box.sw, qt) + (uint32_t)(c0 * 2 / box.sw * (qt * box.sw / 16));
+    const uint32_t uq = qtile / 16, idesc = tc_idesc_16(128, dn, kBf16, 0, 1);
     for (int i = 0; i < tiles; ++i) {
       const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt;
       landed(&q_full[st], (i / sh.stages) & 1u, bad, a.status);
@@ -589,8 +652,8 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
       __syncwarp();
       tc_fence_after_sync();
       if (elect_one()) {
-        mma_steps_ta(acc, tS, dc0 + (st * 2 + 1) * uq, uc, qt / 16, idesc, i > 0);
-        mma_steps_ta(acc + dn, tS + qt, dc0 + st * 2 * uq, uc, qt / 16, idesc, i > 0);
+        mma_over_rows(acc, tS, dc0 + (st * 2 + 1) * uq, box.sw, qt / 16, idesc, i > 0);
+        mma_over_rows(acc + dn, tS + qt, dc0 + st * 2 * uq, box.sw, qt / 16, idesc, i > 0);
         tc_commit(&q_empty[st]);
         tc_commit(&s_free[s]);
         if (i == tiles - 1) tc_commit(&done);
@@ -659,6 +722,10 @@ Plan plan(const AttnArgs& a) {
   // dq: two groups of softmax warps where S, dP and dQ of both fit TMEM with key tiles of 48 or more
   DqShape& s = p.dq;
   s.d16 = d16;
+  s.box = box_of(a.D);
+  s.obox = out_box_of(a.D);
+  const int R = a.H / a.J;
+  s.o_bulk = 32 % R == 0;
   s.tiles = (int)((rows + 127) / 128);
   p.nwg = 2;
   s.kt = ((256 - d16) / 2) & ~15;
@@ -672,7 +739,9 @@ Plan plan(const AttnArgs& a) {
   s.qbufs = 2;
   s.stages = 2;
   const auto dq_smem = [&] {
-    return ((size_t)s.qbufs * p.nwg * 256 + 2 * (size_t)s.stages * s.kt) * d16 * 2 + (size_t)p.nwg * 128 * (s.su | 1) * 16;
+    const size_t manual = (s.su | 1) * 16, bulk = s.obox.wide * 2;
+    return ((size_t)s.qbufs * p.nwg * 256 + 2 * (size_t)s.stages * s.kt) * s.box.row_bytes() +
+           (size_t)p.nwg * 128 * (s.o_bulk && bulk > manual ? bulk : manual);
   };
   while (dq_smem() > kSmemMost) {
     if (s.qbufs == 2) s.qbufs = 1;
@@ -690,12 +759,13 @@ Plan plan(const AttnArgs& a) {
   // dk, dv
   DkvShape& v = p.kv;
   v.d16 = d16;
+  v.box = s.box;
   v.halves = d16 > 192 ? 2 : 1;
-  const int dn = (d16 / 16 + v.halves - 1) / v.halves * 16;
+  const int dn = half_columns(d16, v.halves);
   v.qt = (512 - 2 * dn) / 4 & ~15;
   if (v.qt > 64) v.qt = 64;
   v.stages = kDkvStages;
-  const auto kv_smem = [&] { return (2 * (size_t)kKeyTile + (size_t)v.stages * 2 * v.qt) * d16 * 2; };
+  const auto kv_smem = [&] { return (2 * (size_t)kKeyTile + (size_t)v.stages * 2 * v.qt) * v.box.row_bytes(); };
   while (kv_smem() > kSmemMost - 2048) {
     if (v.stages > 2) --v.stages;
     else v.qt -= 16;
@@ -726,12 +796,33 @@ Plan plan(const AttnArgs& a) {
   return p;
 }
 
+// Maps of q and dout with boxes of `rows` rows of a key head; of k and v with boxes of `rows` keys.
+bool query_maps(Maps* m, const AttnArgs& a, Box box, int rows) {
+  const int R = a.H / a.J, w = box.sw / 2;
+  return rows % R == 0 &&
+         make_map(&m->q, a.dtype, a.q, a.D, a.H, a.Q, a.N, a.qs.head, a.qs.token, a.qs.item, w, R, rows / R, box.sw) &&
+         make_map(&m->dout, a.dtype, a.dout, a.D, a.H, a.Q, a.N, a.dos.head, a.dos.token, a.dos.item, w, R, rows / R, box.sw);
+}
+bool key_maps(Maps* m, const AttnArgs& a, const Keys& keys, Box box, int rows) {
+  const int w = box.sw / 2;
+  return !keys.list &&
+         make_map(&m->k, a.dtype, a.k, a.D, a.J, a.K, a.G, a.ks.head, a.ks.token, a.ks.item, w, 1, rows, box.sw) &&
+         make_map(&m->v, a.dtype, a.v, a.D, a.J, a.K, a.G, a.vs.head, a.vs.token, a.vs.item, w, 1, rows, box.sw);
+}
+
 template <typename T, int NWG>
 cudaError_t go_dq(const AttnArgs& a, const Keys& keys, const Plan& p, float2* stat, cudaStream_t st) {
   static SmemGranted granted;
   const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_dq<T, NWG>), p.dq_smem, granted);
   if (e != cudaSuccess) return e;
-  return launch_ex(k_attn_dq<T, NWG>, dim3(p.grid), dim3(dq_threads<NWG>()), p.dq_smem, st, 0, a, keys, p.dq, stat);
+  Maps m;
+  DqShape s = p.dq;
+  s.q_bulk = query_maps(&m, a, s.box, 128);
+  s.k_bulk = key_maps(&m, a, keys, s.box, s.kt);
+  const int R = a.H / a.J;
+  s.o_bulk = s.o_bulk && make_map(&m.out, a.dtype, a.dq, a.D, a.H, a.Q, a.N, a.dqs.head, a.dqs.token, a.dqs.item, s.obox.wide, R,
+                                  32 / R, s.obox.sw);
+  return launch_ex(k_attn_dq<T, NWG>, dim3(p.grid), dim3(dq_threads<NWG>()), p.dq_smem, st, 0, m, a, keys, s, stat);
 }
 
 template <typename T>
@@ -769,7 +860,11 @@ cudaError_t run(const AttnArgs& a, cudaStream_t st) {
   e = allow_smem(reinterpret_cast<const void*>(k_attn_dkv<T>), p.kv_smem, granted);
   if (e != cudaSuccess) return e;
   const int64_t grid = (int64_t)a.G * a.J * p.kv.kb * p.kv.halves * p.kv.parts;
-  e = launch_ex(k_attn_dkv<T>, dim3((unsigned)grid), dim3(kDkvThreads), p.kv_smem, st, 0, a, keys, p.kv, (const float2*)stat,
+  Maps m;
+  DkvShape v = p.kv;
+  v.q_bulk = (int64_t)a.Q * (a.H / a.J) % v.qt == 0 && query_maps(&m, a, v.box, v.qt);  // no tile of two items
+  v.k_bulk = key_maps(&m, a, keys, v.box, kKeyTile);
+  e = launch_ex(k_attn_dkv<T>, dim3((unsigned)grid), dim3(kDkvThreads), p.kv_smem, st, 0, m, a, keys, v, (const float2*)stat,
                 (const int32_t*)first, (const int32_t*)order, part);
   if (e != cudaSuccess) return e;
   const int64_t ctas = (pieces + 255) / 256;

@@ -39,6 +39,9 @@ struct __align__(16) Work {
 };
 
 struct TcShape {
+  Box box;
+  OutBox obox;
+  bool q_bulk, k_bulk, o_bulk;  // by tiled bulk copies
   int kt, d16, stages, qbufs, splits;
   int tiles, groups;  // query tiles of an item and key head; groups of NWG of them
   uint32_t tmem;      // columns allocated
@@ -58,9 +61,10 @@ __host__ __device__ constexpr int tc_threads() {
 
 template <typename T, int NWG, int L>
 __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
-    k_attn_tc(AttnArgs a, Keys keys, TcShape sh, float* __restrict__ po, float* __restrict__ pl) {
+    k_attn_tc(const __grid_constant__ Maps maps, AttnArgs a, Keys keys, TcShape sh, float* __restrict__ po,
+              float* __restrict__ pl) {
   constexpr int kBf16 = Elem<T>::kBf16, LT = tc_load<NWG>();
-  extern __shared__ __align__(128) unsigned char smem[];
+  extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[kStages], k_empty[kStages], v_full[kStages],
       v_empty[kStages], s_full[NWG][L], p_full[NWG][L], o_full[NWG];
   __shared__ uint32_t s_taddr;
@@ -68,7 +72,8 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   __shared__ int64_t s_rows[2][128];
   const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const int D = a.D, d16 = sh.d16, R = a.H / a.J, kt = sh.kt;
-  const uint32_t qtile = 128u * d16 * 2, ktile = (uint32_t)kt * d16 * 2, cols = L * kt + d16;
+  const Box box = sh.box;
+  const uint32_t qtile = 128u * box.row_bytes(), ktile = (uint32_t)kt * box.row_bytes(), cols = L * kt + d16;
   unsigned char* sq = smem;
   unsigned char* sk = sq + sh.qbufs * NWG * qtile;
   unsigned char* sv = sk + sh.stages * ktile;
@@ -93,11 +98,9 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
     }
     fence_barrier_init();
   }
-  if (D & 8) {  // the columns beyond D, once: no copy touches them
-    const int rows = sh.qbufs * NWG * 128 + 2 * sh.stages * kt;
-    for (int r = tid; r < rows; r += tc_threads<NWG>())
-      *reinterpret_cast<uint4*>(smem + (uint32_t)(r >> 3) * d16 * 16 + (d16 / 8 - 1) * 128 + (r & 7) * 16) =
-          make_uint4(0, 0, 0, 0);
+  if (D != box.row_bytes() / 2 && !(sh.q_bulk && sh.k_bulk && !a.len)) {  // the columns beyond D, once: no copy writes anything else there
+    const uint32_t bytes = (sh.qbufs * NWG) * qtile + 2 * sh.stages * ktile;
+    for (uint32_t o = tid * 16; o < bytes; o += tc_threads<NWG>() * 16) *reinterpret_cast<uint4*>(smem + o) = make_uint4(0, 0, 0, 0);
     fence_proxy_async_smem();
   }
   if (warp == 0) {
@@ -150,10 +153,11 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
     const float c2 = a.scale * kLog2e;
     const int su = stage_units(D), sstride = su | 1;
     const uint32_t usu = 65536u / su + 1;
-    unsigned char* stage = so + warp * 32 * sstride * 16;
+    unsigned char* stage = so + warp * (sh.o_bulk ? 32 * sh.obox.wide * 2 : 32 * sstride * 16);
     uint32_t sc = 0;  // key tiles of this group so far
     struct Pending {  // a work item whose O is to be written
-      int64_t off, row;  // this thread's row: in out (elements), among all rows; negative: none
+      int64_t off, row;  // this thread's row: in out (elements; by bulk copies: the item, head and token of the
+      int head, token;   // warp's first row), among all rows; negative: none
       int part;
       float m, l;
     } pend;
@@ -186,7 +190,10 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         return;
       }
       if (f.row >= 0 && a.lse) a.lse[f.row] = l2 * kLn2;
-      rows_out<T>((T*)a.o, f.off, tO, D, scale, empty, stage, su, sstride, usu, lane);
+      if (sh.o_bulk)
+        rows_out_bulk<T>(&maps.out, f.head, f.token, (int)f.off, f.token < a.Q, tO, D, sh.obox, scale, empty, stage, lane);
+      else
+        rows_out<T>((T*)a.o, f.off, tO, D, scale, empty, stage, su, sstride, usu, lane);
     };
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
       const Work k = work(i, w);
@@ -197,8 +204,14 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         const uint32_t m = (uint32_t)tile * 128 + (warp & 3) * 32 + lane;
         const uint32_t t = R == 1 ? m : m / (uint32_t)R, h = k.j * R + (R == 1 ? 0 : m - t * R);
         const bool there = t < (uint32_t)a.Q;
-        cur.off = there ? k.n * a.os.item + t * a.os.token + h * a.os.head : -1;
         cur.row = there ? ((int64_t)k.n * a.Q + t) * a.H + h : -1;
+        if (sh.o_bulk) {
+          cur.off = k.n;
+          cur.head = k.j * R;
+          cur.token = uniform((int)t);
+        } else {
+          cur.off = there ? k.n * a.os.item + t * a.os.token + h * a.os.head : -1;
+        }
         cur.part = k.part;
       }
       if (k.cnt <= 0) {
@@ -308,6 +321,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       pending = true;
     }
     if (pending) finish(pend, false, sc);
+    if (lane == 0) bulk_stores_done();
   } else if (warp < 4 * NWG + LT / 32) {
     // ================= loads =================
     const int lt = tid - 4 * NWG * 32;
@@ -324,17 +338,21 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       hcnt = k.cnt;
       const T* kp = (const T*)a.k + k.g * a.ks.item + k.j * a.ks.head;
       const T* vp = (const T*)a.v + k.g * a.vs.item + k.j * a.vs.head;
-      auto key_tile = [&](const T* base, int64_t step, unsigned char* to, int k0) {
+      auto key_tile = [&](const T* base, int64_t step, const CUtensorMap* map, unsigned char* to, int k0, uint64_t* bar) {
         const int n = min(kt, k.cnt - k0);
-        copy_keys<LT, T>(tab, smem_u32(to), base, step, keys, k.g, k.lo + k0, n, (n + 15) & ~15, D, d16, lt);
+        if (sh.k_bulk && (n == kt || !a.len)) {  // past a source's length lies anything: not by whole tiles
+          if (bulk_job(bar, ktile, lt)) bulk_tile(smem_u32(to), map, box, kt, k.j, k.lo + k0, k.g, bar);
+          return;
+        }
+        copy_keys<LT, T>(tab, smem_u32(to), base, step, keys, k.g, k.lo + k0, n, (n + 15) & ~15, kt, D, box, lt);
+        copies_arrive(bar);
       };
       const uint32_t qb = qi % sh.qbufs;
       for (int k0 = 0; k0 < k.cnt; k0 += kt) {
         uint32_t st = it % sh.stages;
         if (!reuse) {
           if (it >= (uint32_t)sh.stages) wait_or_bad(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
-          key_tile(kp, a.ks.token, sk + st * ktile, k0);
-          copies_arrive(&k_full[st]);
+          key_tile(kp, a.ks.token, &maps.k, sk + st * ktile, k0, &k_full[st]);
         }
         if (k0 == 0) {
           if (qi >= (uint32_t)sh.qbufs) wait_or_bad(&q_empty[qb], (qi / sh.qbufs - 1) & 1u, bad, a.status);
@@ -342,15 +360,19 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
 #pragma unroll 1
           for (int g = 0; g < NWG; ++g) {
             const int tile = k.group * NWG + g;
-            if (tile < sh.tiles)
-              copy_queries<LT, T>(tab, smem_u32(sq + (qb * NWG + g) * qtile), qp, a.qs, (uint32_t)tile * 128, R, a.Q, D, d16, lt);
+            const uint32_t to = smem_u32(sq + (qb * NWG + g) * qtile);
+            if (tile < sh.tiles && sh.q_bulk) {
+              if (bulk_job(&q_full[qb][g], qtile, lt))
+                bulk_tile(to, &maps.q, box, 128, k.j * R, tile * 128 / R, k.n, &q_full[qb][g]);
+              continue;
+            }
+            if (tile < sh.tiles) copy_queries<LT, T>(tab, to, qp, a.qs, (uint32_t)tile * 128, R, a.Q, D, box, lt);
             copies_arrive(&q_full[qb][g]);
           }
         }
         if (!reuse) {
           if (it >= (uint32_t)sh.stages) wait_or_bad(&v_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
-          key_tile(vp, a.vs.token, sv + st * ktile, k0);
-          copies_arrive(&v_full[st]);
+          key_tile(vp, a.vs.token, &maps.v, sv + st * ktile, k0, &v_full[st]);
           ++it;
         }
       }
@@ -360,8 +382,8 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   } else {
     // ================= MMAs of one group =================
     const int g = uniform(warp - 4 * NWG - LT / 32);
-    const uint64_t dq0 = tile_desc_rows(smem_u32(sq) + g * qtile, d16), dk0 = tile_desc_rows(smem_u32(sk), d16),
-                   dv0 = tile_desc_cols(smem_u32(sv), d16);
+    const uint64_t dq0 = tile_desc_rows(smem_u32(sq) + g * qtile, box.sw), dk0 = tile_desc_rows(smem_u32(sk), box.sw),
+                   dv0 = tile_desc_cols(smem_u32(sv), box.sw, kt);
     const uint32_t uq = NWG * qtile / 16, uk = ktile / 16, t0 = taddr + (uint32_t)g * cols;
     const uint32_t idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
     uint32_t it = 0, qi = 0, sc = 0, v_seen = 0;  // key tiles loaded, work items, key tiles of this group, tiles of V waited for
@@ -384,7 +406,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         __syncwarp();
         tc_fence_after_sync();
         if (elect_one()) {
-          mma_steps_ta(t0 + L * kt, t0 + b * kt, dv0 + e.st * uk, d16 * 2, e.n16 / 16, idesc2, !e.first);
+          mma_over_rows(t0 + L * kt, t0 + b * kt, dv0 + e.st * uk, box.sw, e.n16 / 16, idesc2, !e.first);
           tc_commit(&o_full[g]);
           if (e.release) tc_commit(&v_empty[e.st]);
         }
@@ -436,8 +458,8 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         if (elect_one()) {
           if (valid) {
             const uint32_t b = L == 1 ? 0 : sc & 1u;
-            mma_steps(t0 + b * kt, dq0 + qb * uq, 16, dk0 + s.st * uk, 16, d16 / 16, tc_idesc_16(128, s.n16, kBf16, 0, 0),
-                      false);
+            mma_over_d(t0 + b * kt, dq0 + qb * uq, 128, dk0 + s.st * uk, kt, box.sw, d16 / 16,
+                       tc_idesc_16(128, s.n16, kBf16, 0, 0));
             tc_commit(&s_full[g][b]);
           }
           if (k.cnt > kt) tc_commit(&k_empty[s.st]);
@@ -469,15 +491,19 @@ constexpr int kSms = 152;
 constexpr size_t kSmemMost = 220 << 10;
 
 size_t tc_smem(int nwg, const TcShape& sh, int D) {
-  const size_t row = (size_t)sh.d16 * 2;
-  return ((size_t)sh.qbufs * nwg * 128 + 2 * (size_t)sh.stages * sh.kt) * row +
-         (size_t)nwg * 128 * (stage_units(D) | 1) * 16;
+  const size_t row = sh.box.row_bytes(), manual = (stage_units(D) | 1) * 16, bulk = sh.obox.wide * 2;
+  const size_t stage = sh.o_bulk && bulk > manual ? bulk : manual;  // a map may turn out not to be possible
+  return ((size_t)sh.qbufs * nwg * 128 + 2 * (size_t)sh.stages * sh.kt) * row + (size_t)nwg * 128 * stage;
 }
 
 TcPlan tc_plan(const AttnArgs& a) {
   TcPlan p{};
   TcShape& s = p.sh;
   s.d16 = (a.D + 15) & ~15;
+  s.box = box_of(a.D);
+  s.obox = out_box_of(a.D);
+  const int R = a.H / a.J;
+  s.o_bulk = 32 % R == 0;
   const int64_t rows = (int64_t)a.Q * (a.H / a.J);
   s.tiles = (int)((rows + 127) / 128);
   const int k16 = (a.K + 15) & ~15;
@@ -519,7 +545,16 @@ cudaError_t go(const AttnArgs& a, const Keys& keys, const TcPlan& p, float* po, 
   static SmemGranted granted;
   const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_attn_tc<T, NWG, L>), p.smem, granted);
   if (e != cudaSuccess) return e;
-  return launch_ex(k_attn_tc<T, NWG, L>, dim3(p.grid), dim3(tc_threads<NWG>()), p.smem, st, 0, a, keys, p.sh, po, pl);
+  Maps m;
+  TcShape s = p.sh;
+  const int R = a.H / a.J, sw = s.box.sw, w = sw / 2;
+  s.q_bulk = 128 % R == 0 &&
+             make_map(&m.q, a.dtype, a.q, a.D, a.H, a.Q, a.N, a.qs.head, a.qs.token, a.qs.item, w, R, 128 / R, sw);
+  s.k_bulk = !keys.list && make_map(&m.k, a.dtype, a.k, a.D, a.J, a.K, a.G, a.ks.head, a.ks.token, a.ks.item, w, 1, s.kt, sw) &&
+             make_map(&m.v, a.dtype, a.v, a.D, a.J, a.K, a.G, a.vs.head, a.vs.token, a.vs.item, w, 1, s.kt, sw);
+  s.o_bulk = s.o_bulk && make_map(&m.out, a.dtype, a.o, a.D, a.H, a.Q, a.N, a.os.head, a.os.token, a.os.item, s.obox.wide, R,
+                                  32 / R, s.obox.sw);
+  return launch_ex(k_attn_tc<T, NWG, L>, dim3(p.grid), dim3(tc_threads<NWG>()), p.smem, st, 0, m, a, keys, s, po, pl);
 }
 
 template <typename T>

@@ -2,6 +2,8 @@
 // places of rows, and the join of parts of a softmax.
 #pragma once
 
+#include <cuda.h>
+
 #include "pa_bulk.cuh"
 #include "pa_layers.h"
 #include "pa_tcgen05.cuh"
@@ -104,6 +106,177 @@ __device__ __forceinline__ void columns2(uint32_t t, uint32_t u, int n16, F f) {
     if (c < n16) column_block2<16>(t, u, c, f);
 }
 
+// ---- tensor-core kernels: operand tiles and their copies ---------------------
+// A tile of rows [row][d] lies in shared memory as `blocks` column blocks [row][sw
+// bytes], swizzled (16-byte pieces of eight rows permuted so that neither copies
+// nor MMAs meet bank conflicts; sw: 32, 64 or 128): one layout in which the rows are
+// M or N and d is K, or d is N and the rows are K, and what a tiled bulk copy writes.
+// Columns past d are zeros.
+struct Box {
+  int sw, blocks;
+  __host__ __device__ int row_bytes() const { return sw * blocks; }
+};
+__host__ __device__ inline Box box_of(int D) {  // the least padding, then the widest blocks
+  if (D <= 16) return {32, 1};
+  const int b128 = (D + 63) / 64, b64 = (D + 31) / 32;
+  return b64 * 64 < b128 * 128 ? Box{64, b64} : Box{128, b128};
+}
+__device__ __forceinline__ uint32_t swizzled(uint32_t off, int sw) { return off ^ (((off >> 7) & (uint32_t)(sw / 16 - 1)) << 4); }
+
+__device__ __forceinline__ uint64_t tile_desc(uint32_t base, int sw, uint32_t lbo) {
+  return (uint64_t)((base & 0x3FFFFu) >> 4) | (uint64_t)lbo << 16 | (uint64_t)(uint32_t)(sw / 2) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)(sw == 128 ? 2 : sw == 64 ? 4 : 6) << 61;
+}
+// rows: M or N; d: K. d: N, rows: K (of a tile of `rows` rows).
+__device__ __forceinline__ uint64_t tile_desc_rows(uint32_t base, int sw) { return tile_desc(base, sw, 1); }
+__device__ __forceinline__ uint64_t tile_desc_cols(uint32_t base, int sw, int rows) {
+  return tile_desc(base, sw, (uint32_t)(rows * sw / 16));
+}
+
+// MMAs of one thread. Over d: n steps of 16 of two tiles of ra and rb rows. Over
+// the rows: n steps of 16 rows, A in TMEM (a step is eight columns).
+__device__ __forceinline__ void mma_over_d(uint32_t d, uint64_t a, int ra, uint64_t b, int rb, int sw, int n, uint32_t idesc) {
+  const int per = sw / 32;
+  for (int k = 0; k < n; a += (uint32_t)(ra * sw / 16), b += (uint32_t)(rb * sw / 16))
+    for (int i = 0; i < per && k < n; ++i, ++k) tc_mma_f16(d, a + 2 * i, b + 2 * i, idesc, k > 0 ? 1u : 0u);
+}
+__device__ __forceinline__ void mma_over_rows(uint32_t d, uint32_t a, uint64_t b, int sw, int n, uint32_t idesc, bool add) {
+  for (int k = 0; k < n; ++k, a += 8, b += (uint32_t)sw) tc_mma_f16_ta(d, a, b, idesc, add || k > 0 ? 1u : 0u);
+}
+
+// Bounded wait (about a second); after a failure a thread no longer waits, runs
+// on with accesses in bounds, and the call's results are not valid.
+__device__ __forceinline__ void wait_or_bad(uint64_t* bar, uint32_t parity, bool& bad, int32_t* status) {
+  if (bad || mbar_test(bar, parity)) return;
+  const long long t0 = clock64();
+  while (!mbar_try(bar, parity)) {
+    if (clock64() - t0 > 2000000000ll) {
+      bad = true;
+      atomicCAS(status, 0, kDevTimeout);
+      return;
+    }
+  }
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
+// The loader threads' copies of a job land some time later; its mbarrier then
+// gets each thread's arrival. Whoever waits for them to issue MMAs makes them
+// visible to the tensor core (landed).
+__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void copies_drain() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void landed(uint64_t* bar, uint32_t parity, bool& bad, int32_t* status) {
+  wait_or_bad(bar, parity, bad, status);
+  fence_proxy_async_smem();
+}
+
+// Tiled bulk copies: an output or input [item][token][head][d] as a tensor map
+// over (d, head, token, item); a box is `sw` bytes x heads x tokens.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const CUtensorMap* map, int x, int head, int token, int item,
+                                          uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
+          dst),
+      "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(head), "r"(token), "r"(item)
+      : "memory");
+}
+__device__ __forceinline__ void bulk_store(const CUtensorMap* map, uint32_t src, int x, int head, int token, int item) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map), "r"(src),
+               "r"(x), "r"(head), "r"(token), "r"(item)
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void bulk_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+// A whole tile of `rows` rows, by one thread.
+__device__ __forceinline__ void bulk_tile(uint32_t dst, const CUtensorMap* map, Box box, int rows, int head, int token, int item,
+                                          uint64_t* bar) {
+  for (int b = 0; b < box.blocks; ++b, dst += (uint32_t)(rows * box.sw)) bulk_load(dst, map, b * (box.sw / 2), head, token, item, bar);
+}
+
+// Copy `rows` (a multiple of 8) rows of a tile of `tall` rows by LT threads, 16
+// bytes at a time, row r from at(r) on (NULL: zeros). Eight neighbouring threads
+// take a piece of eight rows, neighbouring eights neighbouring pieces.
+template <int LT, typename T, typename At>
+__device__ __forceinline__ void copy_rows(uint32_t dst, int rows, int tall, int d, Box box, const T* any, int tid, At at) {
+  const int nch = d >> 3, per = box.sw >> 4, lg = 31 - __clz(per);
+  int c = tid >> 3, row = tid & 7;
+  row += c / nch * 8;
+  c %= nch;
+  const int dc = (LT / 8) % nch, dr = (LT / 8) / nch * 8;
+#pragma unroll 2
+  while (row < rows) {
+    const T* p = at(row);
+    const uint32_t to = dst + (uint32_t)((c >> lg) * tall * box.sw) +
+                        swizzled((uint32_t)(row * box.sw + (c & (per - 1)) * 16), box.sw);
+    copy16(to, p ? p + c * 8 : any, p != nullptr);
+    c += dc;
+    row += dr;
+    if (c >= nch) {
+      c -= nch;
+      row += 8;
+    }
+  }
+}
+
+// What the loader threads share: a table of row offsets, two in turn (a thread
+// that fills one has seen every thread pass the barrier after the other's use).
+template <int LT>
+struct RowTables {
+  int64_t (*at)[128];
+  int turn;
+  // off(r): element offset of row r, negative: zeros
+  template <typename F>
+  __device__ __forceinline__ const int64_t* fill(int rows, int tid, F off) {
+    int64_t* t = at[turn ^= 1];
+    for (int r = tid; r < rows; r += LT) t[r] = off(r);
+    asm volatile("bar.sync 1, %0;" ::"n"(LT) : "memory");
+    return t;
+  }
+};
+
+// A job of all loader threads behind one mbarrier that counts them: a tile of
+// rows by a tiled bulk copy where `map` holds, else piece by piece.
+//
+// Rows m0 .. m0 + 127 of an item and key head (m = token x R + head of the key
+// head), zeros past the last token.
+template <int LT, typename T>
+__device__ __forceinline__ void copy_queries(RowTables<LT>& tab, uint32_t dst, const T* base, const Strides& s, uint32_t m0,
+                                             int R, int Q, int d, Box box, int tid) {
+  const int64_t* off = tab.fill(128, tid, [&](int r) {
+    const uint32_t m = m0 + r, t = R == 1 ? m : m / (uint32_t)R;
+    return t < (uint32_t)Q ? t * s.token + (m - t * R) * s.head : (int64_t)-1;
+  });
+  copy_rows<LT, T>(dst, 128, 128, d, box, base, tid, [&](int r) { return off[r] < 0 ? (const T*)nullptr : base + off[r]; });
+}
+// Keys k0 .. k0 + n - 1 of a source's keys that count, zeros up to `rows`.
+template <int LT, typename T>
+__device__ __forceinline__ void copy_keys(RowTables<LT>& tab, uint32_t dst, const T* base, int64_t stride, const Keys& keys, int g,
+                                          int k0, int n, int rows, int tall, int d, Box box, int tid) {
+  if (!keys.list) {
+    const T* first = base + k0 * stride;
+    copy_rows<LT, T>(dst, rows, tall, d, box, base, tid, [&](int r) { return r < n ? first + r * stride : (const T*)nullptr; });
+    return;
+  }
+  const int64_t* off = tab.fill(rows, tid, [&](int r) { return r < n ? keys.at(g, k0 + r) * stride : (int64_t)-1; });
+  copy_rows<LT, T>(dst, rows, tall, d, box, base, tid, [&](int r) { return off[r] < 0 ? (const T*)nullptr : base + off[r]; });
+}
+// The arrivals for a tile of `bytes` that thread 0 fetches by bulk copies; it
+// issues them when this says so.
+__device__ __forceinline__ bool bulk_job(uint64_t* bar, uint32_t bytes, int tid) {
+  if (tid == 0) {
+    fence_proxy_async_smem();  // the buffer may have been written piece by piece before
+    mbar_arrive_expect_tx(bar, bytes);
+    return true;
+  }
+  mbar_arrive(bar);
+  return false;
+}
+
 // A warp's 32 rows of a tile, `scale` times the D columns from t on, to memory in
 // 16 bits: staged in shared memory (su 16-byte units of a row at a time, sstride
 // units apart; usu = 65536 / su + 1), then neighbouring lanes write neighbouring
@@ -138,156 +311,56 @@ __device__ __forceinline__ void rows_out(T* to, int64_t off, uint32_t t, int D, 
   }
 }
 
-// ---- tensor-core kernels: operand tiles and their copies ---------------------
-// A tile of rows [row][d] lies in shared memory as core matrices of 8 rows x 16
-// bytes, those of eight rows side by side: one layout in which the rows are M or
-// N and d is K, or d is N (or M) and the rows are K. d16: d rounded up to 16; the
-// last eight columns of it are zeros where d % 16 == 8.
-__device__ __forceinline__ uint64_t tile_desc_rows(uint32_t base, int d16) {  // rows: M or N; d: K
-  return tc_smem_desc(base, 128, (uint32_t)d16 * 16);
-}
-__device__ __forceinline__ uint64_t tile_desc_cols(uint32_t base, int d16) {  // d: M or N; rows: K
-  return tc_smem_desc(base, (uint32_t)d16 * 16, 128);
-}
-
-// n K steps of an MMA from descriptors whose start addresses move by `da`, `db`
-// 16-byte units a step; one thread. With A in TMEM a step is eight columns.
-__device__ __forceinline__ void mma_steps(uint32_t d, uint64_t a, uint32_t da, uint64_t b, uint32_t db, int n, uint32_t idesc,
-                                          bool add) {
-  for (int k = 0; k < n; ++k, a += da, b += db) tc_mma_f16(d, a, b, idesc, add || k > 0 ? 1u : 0u);
-}
-__device__ __forceinline__ void mma_steps_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t db, int n, uint32_t idesc, bool add) {
-  for (int k = 0; k < n; ++k, a += 8, b += db) tc_mma_f16_ta(d, a, b, idesc, add || k > 0 ? 1u : 0u);
-}
-
-// Bounded wait (about a second); after a failure a thread no longer waits, runs
-// on with accesses in bounds, and the call's results are not valid.
-__device__ __forceinline__ void wait_or_bad(uint64_t* bar, uint32_t parity, bool& bad, int32_t* status) {
-  if (bad || mbar_test(bar, parity)) return;
-  const long long t0 = clock64();
-  while (!mbar_try(bar, parity)) {
-    if (clock64() - t0 > 2000000000ll) {
-      bad = true;
-      atomicCAS(status, 0, kDevTimeout);
-      return;
-    }
-  }
-}
-
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-
-// The loader threads' copies of a job land some time later; its mbarrier then
-// gets each thread's arrival. Whoever waits for them to issue MMAs makes them
-// visible to the tensor core (landed).
-__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void copies_drain() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-__device__ __forceinline__ void landed(uint64_t* bar, uint32_t parity, bool& bad, int32_t* status) {
-  wait_or_bad(bar, parity, bad, status);
-  fence_proxy_async_smem();
-}
-
-// Copy `rows` (a multiple of 8) rows of a tile by LT threads, zeros from row
-// `valid` on. Eight neighbouring threads fill a core matrix; neighbouring groups
-// of eight take neighbouring 16-byte pieces of the same eight rows. Rows at one
-// distance: pointers only ever step.
-template <int LT, typename T>
-__device__ __forceinline__ void copy_rows(uint32_t dst, int rows, int valid, int d, int d16, const T* base, int64_t stride,
-                                          int tid) {
-  const int nch = d >> 3;
-  int c = tid >> 3, row = tid & 7;
-  row += c / nch * 8;
-  c %= nch;
-  const T* p = base + row * stride + c * 8;
-  dst += (uint32_t)(row >> 3) * d16 * 16 + c * 128 + (row & 7) * 16;
-  const int dc = (LT / 8) % nch, dr = (LT / 8) / nch * 8;
-  const int64_t dp = dr * stride + dc * 8, wp = 8 * stride - nch * 8;
-  const uint32_t dd = (uint32_t)(dr >> 3) * d16 * 16 + dc * 128, wd = (uint32_t)d16 * 16 - nch * 128;
-#pragma unroll 2
-  while (row < rows) {
-    copy16(dst, row < valid ? p : base, row < valid);
-    c += dc;
-    row += dr;
-    p += dp;
-    dst += dd;
-    if (c >= nch) {
-      c -= nch;
-      row += 8;
-      p += wp;
-      dst += wd;
-    }
-  }
-}
-// Rows at offsets (in elements, negative: zeros) that a table in shared memory holds.
-template <int LT, typename T>
-__device__ __forceinline__ void copy_rows_at(uint32_t dst, int rows, int d, int d16, const T* base, const int64_t* off, int tid) {
-  const int nch = d >> 3;
-  int c = tid >> 3, row = tid & 7;
-  row += c / nch * 8;
-  c %= nch;
-  dst += (uint32_t)(row >> 3) * d16 * 16 + c * 128 + (row & 7) * 16;
-  const int dc = (LT / 8) % nch, dr = (LT / 8) / nch * 8;
-  const uint32_t dd = (uint32_t)(dr >> 3) * d16 * 16 + dc * 128, wd = (uint32_t)d16 * 16 - nch * 128;
-#pragma unroll 2
-  while (row < rows) {
-    const int64_t o = off[row];
-    copy16(dst, base + (o < 0 ? 0 : o + c * 8), o >= 0);
-    c += dc;
-    row += dr;
-    dst += dd;
-    if (c >= nch) {
-      c -= nch;
-      row += 8;
-      dst += wd;
-    }
-  }
-}
-
-// What the loader threads share: a table of row offsets, two in turn (a thread
-// that fills one has seen every thread pass the barrier after the other's use).
-template <int LT>
-struct RowTables {
-  int64_t (*at)[128];
-  int turn;
-  // off(r): element offset of row r, negative: zeros
-  template <typename F>
-  __device__ __forceinline__ const int64_t* fill(int rows, int tid, F off) {
-    int64_t* t = at[turn ^= 1];
-    for (int r = tid; r < rows; r += LT) t[r] = off(r);
-    asm volatile("bar.sync 1, %0;" ::"n"(LT) : "memory");
-    return t;
-  }
+// The same by tiled bulk stores, one per `wide` columns: the warp's rows staged as
+// the box of the map (rows of 2 D bytes, or swizzled rows of sw bytes), rows past
+// the last token are left out by the copy.
+struct OutBox {
+  int wide, sw;  // columns of a box; swizzle (0: none)
 };
+__host__ __device__ inline OutBox out_box_of(int D) {  // dense rows meet no bank conflicts for odd D / 8
+  if (D / 8 % 2 == 1) return {D, 0};
+  const Box b = box_of(D);
+  return {b.sw / 2, b.sw};
+}
+template <typename T>
+__device__ __forceinline__ void rows_out_bulk(const CUtensorMap* map, int head, int token, int item, bool there, uint32_t t, int D,
+                                              OutBox box, float scale, bool zero, unsigned char* stage, int lane) {
+  const int pitch = box.wide * 2;
+  for (int c0 = 0; c0 < D; c0 += box.wide) {
+    const int cols = min(box.wide, D - c0);
+    if (lane == 0) bulk_stores_read();  // the stage may be written again
+    __syncwarp();
+    auto put = [&](int c, uint4 v) {
+      const uint32_t off = (uint32_t)(lane * pitch + c * 2);
+      *reinterpret_cast<uint4*>(stage + (box.sw ? swizzled(off, box.sw) : off)) = v;
+    };
+    if (zero) {
+      for (int c = 0; c < cols; c += 8) put(c, make_uint4(0, 0, 0, 0));
+    } else {
+      columns<16>(t + c0, (cols + 15) & ~15, [&](auto& r, int c) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float v[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(r[8 * h + q]) * scale;
+          if (h == 0 || c + 8 < cols) put(c + 8 * h, Elem<T>::pack(v));
+        }
+      });
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0 && there) bulk_store(map, smem_u32(stage), c0, head, token, item);
+  }
+}
 
-// Rows m0 .. m0 + 127 of an item and key head (m = token x R + head of the key
-// head), zeros past the last token; keys k0 .. k0 + n - 1 of a source's keys
-// that count, zeros up to a multiple of 16.
-template <int LT, typename T>
-__device__ __forceinline__ void copy_queries(RowTables<LT>& tab, uint32_t dst, const T* base, const Strides& s, uint32_t m0,
-                                             int R, int Q, int d, int d16, int tid) {
-  if (R == 1) {
-    copy_rows<LT, T>(dst, 128, min(128, Q - (int)m0), d, d16, base + m0 * s.token, s.token, tid);
-    return;
-  }
-  const int64_t* off = tab.fill(128, tid, [&](int r) {
-    const uint32_t m = m0 + r, t = m / (uint32_t)R;
-    return t < (uint32_t)Q ? t * s.token + (m - t * R) * s.head : (int64_t)-1;
-  });
-  copy_rows_at<LT, T>(dst, 128, d, d16, base, off, tid);
-}
-template <int LT, typename T>
-__device__ __forceinline__ void copy_keys(RowTables<LT>& tab, uint32_t dst, const T* base, int64_t stride, const Keys& keys, int g,
-                                          int k0, int n, int rows, int d, int d16, int tid) {
-  if (!keys.list) {
-    copy_rows<LT, T>(dst, rows, n, d, d16, base + k0 * stride, stride, tid);
-    return;
-  }
-  const int64_t* off = tab.fill(rows, tid, [&](int r) { return r < n ? keys.at(g, k0 + r) * stride : (int64_t)-1; });
-  copy_rows_at<LT, T>(dst, rows, d, d16, base, off, tid);
-}
+// Tensor maps of a call, made on the host; use: whether the map could be made.
+struct alignas(64) Maps {
+  CUtensorMap q, k, v, out, dout;
+};
+// [n3][n2][n1][D] with strides in elements, boxes of b2 x b1 rows of `cols` columns
+// with swizzle sw; false where the shape or the strides have no such map.
+bool make_map(CUtensorMap* map, int dtype, const void* base, int D, int64_t n1, int64_t n2, int64_t n3, int64_t s1, int64_t s2,
+              int64_t s3, int cols, int b1, int b2, int sw);
 
 // The list above (k_attn.cu).
 cudaError_t launch_attn_keys(const AttnArgs& a, int32_t* n, int32_t* list, int32_t* pos, cudaStream_t st);
