@@ -364,12 +364,12 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
               __syncwarp();
               if (elect_one()) tc_commit(&k_empty[pst]);
             }
-            landed(&k_full[st], (it / sh.stages) & 1u, bad, a.status);
+            landed(&k_full[st], (it / sh.stages) & 1u, !sh.k_bulk || a.len, bad, a.status);
           }
           if (pv) second();
           pv = valid;
           // without a tile it waits all the same: it must not run ahead of the loaders
-          if (begin) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+          if (begin) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, !sh.q_bulk, bad, a.status);
           if (valid) {
             __syncwarp();
             tc_fence_after_sync();
@@ -628,10 +628,10 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
     const uint64_t dk0 = tile_desc_rows(smem_u32(sk), box.sw), dv0 = tile_desc_rows(smem_u32(sv), box.sw),
                    dq0 = tile_desc_rows(smem_u32(sq), box.sw);
     const uint32_t uq = qtile / 16, idesc = tc_idesc_16(128, qt, kBf16, 0, 0);
-    if (tiles > 0) landed(&k_full, 0, bad, a.status);
+    if (tiles > 0) landed(&k_full, 0, !sh.k_bulk || a.len, bad, a.status);
     for (int i = 0; i < tiles; ++i) {
       const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt;
-      landed(&q_full[st], (i / sh.stages) & 1u, bad, a.status);
+      landed(&q_full[st], (i / sh.stages) & 1u, !sh.q_bulk, bad, a.status);
       if (i >= 2) wait_or_bad(&s_free[s], (i / 2 - 1) & 1u, bad, a.status);
       __syncwarp();
       tc_fence_after_sync();
@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
     const uint32_t uq = qtile / 16, idesc = tc_idesc_16(128, dn, kBf16, 0, 1);
     for (int i = 0; i < tiles; ++i) {
       const uint32_t st = i % sh.stages, s = i & 1, tS = taddr + s * 2 * qt;
-      landed(&q_full[st], (i / sh.stages) & 1u, bad, a.status);
+      landed(&q_full[st], (i / sh.stages) & 1u, !sh.q_bulk, bad, a.status);
       wait_or_bad(&p_full[s], (i / 2) & 1u, bad, a.status);
       __syncwarp();
       tc_fence_after_sync();

@@ -291,25 +291,28 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
             }
           });
           const float mc = raise(max3(fmaxf(mx[0], mx[1]), mx[2], mx[3]));
-          float sum[4] = {};
+          F2 sum[2] = {F2(0.f, 0.f), F2(0.f, 0.f)};
           columns<32>(tS, n16, [&](auto& r, int c) {
             constexpr int N = sizeof(r) / 4;
             uint32_t p[N / 2];
-            const bool whole = c + N <= n;
+            if (c + N > n) {
+#pragma unroll
+              for (int q = 0; q < N; ++q) r[q] = c + q < n ? r[q] : 0xff800000u;
+            }
 #pragma unroll
             for (int q = 0; q < N; q += 2) {
-              float x = ex2(fmaf(__uint_as_float(r[q]), c2, mc)), y = ex2(fmaf(__uint_as_float(r[q + 1]), c2, mc));
-              if (!whole) {
-                x = c + q < n ? x : 0.f;
-                y = c + q + 1 < n ? y : 0.f;
-              }
-              sum[q & 2] += x;
-              sum[(q & 2) + 1] += y;
+              float x, y;
+              fma2(F2(r[q], r[q + 1]), F2(c2, c2), F2(mc, mc)).get(x, y);
+              x = ex2(x);
+              y = ex2(y);
+              sum[q / 2 & 1] = add2(sum[q / 2 & 1], F2(x, y));
               p[q / 2] = Elem<T>::pack2(x, y);
             }
             tmem_st(tS + c / 2, p);
           });
-          cur.l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          float x, y;
+          add2(sum[0], sum[1]).get(x, y);
+          cur.l += x + y;
         }
         if (k0 == 0 && pending) finish(pend, false, before);
         tmem_st_wait();
@@ -386,6 +389,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
                    dv0 = tile_desc_cols(smem_u32(sv), box.sw, kt);
     const uint32_t uq = NWG * qtile / 16, uk = ktile / 16, t0 = taddr + (uint32_t)g * cols;
     const uint32_t idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
+    const bool k_pieces = !sh.k_bulk || a.len;
     uint32_t it = 0, qi = 0, sc = 0, v_seen = 0;  // key tiles loaded, work items, key tiles of this group, tiles of V waited for
     int hg = -1, hj = 0, hlo = 0, hcnt = 0;
     struct Step {  // a key tile whose S is issued and whose O += P V is not
@@ -400,7 +404,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         const uint32_t b = L == 1 ? 0 : e.sc & 1u;
         wait_or_bad(&p_full[g][b], (e.sc / L) & 1u, bad, a.status);
         if (e.it >= v_seen) {
-          landed(&v_full[e.st], (e.it / sh.stages) & 1u, bad, a.status);
+          landed(&v_full[e.st], (e.it / sh.stages) & 1u, k_pieces, bad, a.status);
           v_seen = e.it + 1;
         }
         __syncwarp();
@@ -444,14 +448,14 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
           }
           s.it = it++;
           s.st = s.it % sh.stages;
-          landed(&k_full[s.st], (s.it / sh.stages) & 1u, bad, a.status);
+          landed(&k_full[s.st], (s.it / sh.stages) & 1u, k_pieces, bad, a.status);
         }
         if (waiting == L) {
           second(L == 1 ? newer : older);
           --waiting;
         }
         // without a tile it waits all the same: it must not run ahead of the loaders
-        if (k0 == 0) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, bad, a.status);
+        if (k0 == 0) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, !sh.q_bulk, bad, a.status);
         s.sc = sc;
         __syncwarp();
         tc_fence_after_sync();

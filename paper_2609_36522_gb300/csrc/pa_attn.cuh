@@ -164,14 +164,15 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
 
 // The loader threads' copies of a job land some time later; its mbarrier then
 // gets each thread's arrival. Whoever waits for them to issue MMAs makes them
-// visible to the tensor core (landed).
+// visible to the tensor core (landed; tiles by bulk copies are visible, and the
+// fence costs hundreds of cycles).
 __device__ __forceinline__ void copies_arrive(uint64_t* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 __device__ __forceinline__ void copies_drain() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-__device__ __forceinline__ void landed(uint64_t* bar, uint32_t parity, bool& bad, int32_t* status) {
+__device__ __forceinline__ void landed(uint64_t* bar, uint32_t parity, bool pieces, bool& bad, int32_t* status) {
   wait_or_bad(bar, parity, bad, status);
-  fence_proxy_async_smem();
+  if (pieces) fence_proxy_async_smem();
 }
 
 // Tiled bulk copies: an output or input [item][token][head][d] as a tensor map
@@ -337,13 +338,14 @@ __device__ __forceinline__ void rows_out_bulk(const CUtensorMap* map, int head, 
     if (zero) {
       for (int c = 0; c < cols; c += 8) put(c, make_uint4(0, 0, 0, 0));
     } else {
-      columns<16>(t + c0, (cols + 15) & ~15, [&](auto& r, int c) {
+      columns<32>(t + c0, (cols + 15) & ~15, [&](auto& r, int c) {
+        constexpr int N = sizeof(r) / 32;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < N; ++h) {
           float v[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) v[q] = __uint_as_float(r[8 * h + q]) * scale;
-          if (h == 0 || c + 8 < cols) put(c + 8 * h, Elem<T>::pack(v));
+          if (h + 1 < N || c + 8 * h < cols) put(c + 8 * h, Elem<T>::pack(v));
         }
       });
     }
@@ -354,7 +356,7 @@ __device__ __forceinline__ void rows_out_bulk(const CUtensorMap* map, int head, 
 }
 
 // Tensor maps of a call, made on the host; use: whether the map could be made.
-struct alignas(64) Maps {
+struct Maps {
   CUtensorMap q, k, v, out, dout;
 };
 // [n3][n2][n1][D] with strides in elements, boxes of b2 x b1 rows of `cols` columns
