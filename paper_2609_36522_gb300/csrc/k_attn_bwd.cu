@@ -70,7 +70,7 @@ struct DqShape {
   Box box;
   OutBox obox;
   bool q_bulk, k_bulk, o_bulk;  // by tiled bulk copies
-  int kt, d16, stages, qbufs, tiles, groups, su;
+  int kt, d16, stages, qbufs, tiles, groups;
   uint32_t tmem;
 };
 constexpr int kTable = 128;  // work items of a CTA that are looked up at the start
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
     const int g = warp >> 2;
     const uint32_t tS = taddr + (uint32_t)g * cols + ((uint32_t)(warp & 3) << 21), tP = tS + kt, tO = tP + kt;
     const float c2 = a.scale * kLog2e;
-    const int su = sh.su, sstride = su | 1;
+    const int su = stage_units(D), sstride = su | 1;
     const uint32_t usu = 65536u / su + 1;
     unsigned char* stage = so + warp * (sh.o_bulk ? 32 * sh.obox.wide * 2 : 32 * sstride * 16);
     uint32_t s_par = 0, o_par = 0;
@@ -735,13 +735,10 @@ Plan plan(const AttnArgs& a) {
   }
   if (s.kt > 128) s.kt = 128;
   if (s.kt > k16) s.kt = k16;
-  s.su = a.D / 8 < 8 ? a.D / 8 : a.D > 64 ? 4 : 8;
   s.qbufs = 2;
   s.stages = 2;
   const auto dq_smem = [&] {
-    const size_t manual = (s.su | 1) * 16, bulk = s.obox.wide * 2;
-    return ((size_t)s.qbufs * p.nwg * 256 + 2 * (size_t)s.stages * s.kt) * s.box.row_bytes() +
-           (size_t)p.nwg * 128 * (s.o_bulk && bulk > manual ? bulk : manual);
+    return ((size_t)s.qbufs * p.nwg * 256 + 2 * (size_t)s.stages * s.kt) * s.box.row_bytes() + (size_t)p.nwg * 4 * stage_bytes(a.D);
   };
   while (dq_smem() > kSmemMost) {
     if (s.qbufs == 2) s.qbufs = 1;

@@ -47,8 +47,6 @@ struct TcShape {
   uint32_t tmem;      // columns allocated
 };
 
-__host__ __device__ inline int stage_units(int D) { return D / 8 < 8 ? D / 8 : 8; }  // 16-byte units of a staged row
-
 // Loader warps fill up to a multiple of four warps (registers are given out by four).
 template <int NWG>
 __host__ __device__ constexpr int tc_load() {
@@ -153,7 +151,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
     const float c2 = a.scale * kLog2e;
     const int su = stage_units(D), sstride = su | 1;
     const uint32_t usu = 65536u / su + 1;
-    unsigned char* stage = so + warp * (sh.o_bulk ? 32 * sh.obox.wide * 2 : 32 * sstride * 16);
+    unsigned char* stage = so + warp * (sh.o_bulk ? 32 * sh.obox.wide * 2 : 32 * sstride * 16);  // (swizzled stages: whole KB)
     uint32_t sc = 0;  // key tiles of this group so far
     struct Pending {  // a work item whose O is to be written
       int64_t off, row;  // this thread's row: in out (elements; by bulk copies: the item, head and token of the
@@ -495,9 +493,8 @@ constexpr int kSms = 152;
 constexpr size_t kSmemMost = 220 << 10;
 
 size_t tc_smem(int nwg, const TcShape& sh, int D) {
-  const size_t row = sh.box.row_bytes(), manual = (stage_units(D) | 1) * 16, bulk = sh.obox.wide * 2;
-  const size_t stage = sh.o_bulk && bulk > manual ? bulk : manual;  // a map may turn out not to be possible
-  return ((size_t)sh.qbufs * nwg * 128 + 2 * (size_t)sh.stages * sh.kt) * row + (size_t)nwg * 128 * stage;
+  const size_t row = sh.box.row_bytes();
+  return ((size_t)sh.qbufs * nwg * 128 + 2 * (size_t)sh.stages * sh.kt) * row + (size_t)nwg * 4 * stage_bytes(D);
 }
 
 TcPlan tc_plan(const AttnArgs& a) {

@@ -318,10 +318,17 @@ __device__ __forceinline__ void rows_out(T* to, int64_t off, uint32_t t, int D, 
 struct OutBox {
   int wide, sw;  // columns of a box; swizzle (0: none)
 };
-__host__ __device__ inline OutBox out_box_of(int D) {  // dense rows meet no bank conflicts for odd D / 8
-  if (D / 8 % 2 == 1) return {D, 0};
+__host__ __device__ inline OutBox out_box_of(int D) {
+  if (D > 64) return {32, 64};          // wide heads: shared memory goes to operand tiles
+  if (D / 8 % 2 == 1) return {D, 0};    // dense rows of an odd number of pieces meet no bank conflicts
   const Box b = box_of(D);
   return {b.sw / 2, b.sw};
+}
+__host__ __device__ inline int stage_units(int D) { return D <= 64 ? D / 8 : 4; }  // 16-byte units of a row staged piece by piece
+// Bytes of a warp's stage for either way out.
+__host__ __device__ inline int stage_bytes(int D) {
+  const int pieces = 32 * (stage_units(D) | 1) * 16, bulk = 32 * out_box_of(D).wide * 2;
+  return pieces > bulk ? pieces : bulk;
 }
 template <typename T>
 __device__ __forceinline__ void rows_out_bulk(const CUtensorMap* map, int head, int token, int item, bool there, uint32_t t, int D,
