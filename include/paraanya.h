@@ -700,7 +700,7 @@ typedef struct {
   const void *q, *k, *v;
   int64_t q_stride[3], k_stride[3], v_stride[3];   /* item (k, v: source), token, head */
   const int32_t* source;       /* DEVICE; an index outside [0, sources) leaves its item without keys */
-  int64_t source_stride;       /* and is reported by pa_attention_check */
+  int64_t source_stride;       /* and is reported by pa_layers_check */
   const int32_t* lengths;      /* DEVICE [sources] */
   const uint8_t* mask;         /* DEVICE [sources][mask_stride] */
   int64_t mask_stride;
@@ -730,11 +730,11 @@ PA_API pa_status pa_attention(const pa_attention_t* a, void* workspace_dev, size
 PA_API pa_status pa_attention_backward(const pa_attention_t* a, void* workspace_dev, size_t workspace_bytes,
                                        void* stream);
 
-/* Synchronise `stream`, report the first device-side failure of the attention
+/* Synchronise `stream`, report the first device-side failure of these layers'
  * calls on this device since the last check, and clear it: PA_ERR_DEVICE for a
  * source index out of range, PA_ERR_TIMEOUT for a bounded wait that ran out
  * (the outputs of that call are not valid). */
-PA_API pa_status pa_attention_check(void* stream);
+PA_API pa_status pa_layers_check(void* stream);
 
 /* ---- misc -------------------------------------------------------------- */
 

@@ -124,7 +124,7 @@ _PROTOS = {
     "pa_attention_workspace_bytes": (C.c_size_t, [VP, C.c_int]),
     "pa_attention": (C.c_int, [VP, VP, C.c_size_t, VP]),
     "pa_attention_backward": (C.c_int, [VP, VP, C.c_size_t, VP]),
-    "pa_attention_check": (C.c_int, [VP]),
+    "pa_layers_check": (C.c_int, [VP]),
     "pa_status_string": (C.c_char_p, [C.c_int]),
     "pa_last_error": (C.c_char_p, []),
 }
@@ -512,5 +512,5 @@ def pa_attention_backward(a, workspace_ptr, workspace_bytes, stream_ptr):
     return _check("pa_attention_backward", lib().pa_attention_backward(a, workspace_ptr, workspace_bytes, stream_ptr))
 
 
-def pa_attention_check(stream_ptr):
-    return _check("pa_attention_check", lib().pa_attention_check(_dptr(stream_ptr)))
+def pa_layers_check(stream_ptr):
+    return _check("pa_layers_check", lib().pa_layers_check(_dptr(stream_ptr)))

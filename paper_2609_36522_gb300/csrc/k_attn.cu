@@ -347,7 +347,7 @@ bool make_map(CUtensorMap* map, int dtype, const void* base, int D, int64_t n1, 
                 CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-cudaError_t attn_status(int32_t** out) {
+cudaError_t layers_status(int32_t** out) {
   static std::atomic<int32_t*> known[64];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);

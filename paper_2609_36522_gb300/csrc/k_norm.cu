@@ -17,7 +17,9 @@
 // each pass. dw and db: each thread sums its columns over its rows in
 // registers, the groups of a CTA are added in a fixed order, and a second kernel
 // adds the CTAs' sums in order: the result does not depend on timing.
+#include "pa_bulk.cuh"
 #include "pa_layers.h"
+#include "pa_wait.cuh"
 
 namespace pa {
 namespace {
@@ -171,6 +173,38 @@ __global__ void __launch_bounds__(CTA ? kCtaThreads : kThreads) k_norm(const T* 
   }
 }
 
+// A CTA's sums of dw and db to part [CTA][2][cols]: the groups of a warp, then the
+// warps one after another. s: [2][cols]. Every thread of the CTA.
+template <int V, int N>
+__device__ __forceinline__ void cta_sums(float (&dw)[N * V], float (&db)[N * V], float* s, int cols, int tpr, int at, float* part) {
+  for (int o = tpr; o < 32; o <<= 1) {
+#pragma unroll
+    for (int q = 0; q < N * V; ++q) {
+      dw[q] += __shfl_xor_sync(0xffffffffu, dw[q], o);
+      db[q] += __shfl_xor_sync(0xffffffffu, db[q], o);
+    }
+  }
+  const int warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+  for (int t = 0; t < nw; ++t) {
+    if (warp == t && (int)(threadIdx.x & 31) < tpr) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = (at + i * tpr) * V;
+        if (c < cols) {
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            s[c + k] = dw[i * V + k] + (t ? s[c + k] : 0.f);
+            s[cols + c + k] = db[i * V + k] + (t ? s[cols + c + k] : 0.f);
+          }
+        }
+      }
+    }
+    __syncthreads();
+  }
+  float* o = part + (int64_t)blockIdx.x * 2 * cols;
+  for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) o[c] = s[c];
+}
+
 // Backward, and a CTA's sums of dw and db (part: [CTA][2][cols]) where SUMS.
 template <typename T, int V, int N, bool CTA, bool SUMS>
 __global__ void __launch_bounds__(CTA ? kCtaThreads : kThreads)
@@ -251,33 +285,7 @@ __global__ void __launch_bounds__(CTA ? kCtaThreads : kThreads)
   }
   if constexpr (SUMS) {
     if constexpr (!CTA) {
-      // the groups of a warp, then the warps one after another
-      for (int o = tpr; o < 32; o <<= 1) {
-#pragma unroll
-        for (int q = 0; q < N * V; ++q) {
-          dw[q] += __shfl_xor_sync(0xffffffffu, dw[q], o);
-          db[q] += __shfl_xor_sync(0xffffffffu, db[q], o);
-        }
-      }
-      const int warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
-      for (int t = 0; t < nw; ++t) {
-        if (warp == t && (int)(threadIdx.x & 31) < tpr) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const int c = (R.at + i * tpr) * V;
-            if (c < cols) {
-#pragma unroll
-              for (int k = 0; k < V; ++k) {
-                s_part[c + k] = dw[i * V + k] + (t ? s_part[c + k] : 0.f);
-                s_part[cols + c + k] = db[i * V + k] + (t ? s_part[cols + c + k] : 0.f);
-              }
-            }
-          }
-        }
-        __syncthreads();
-      }
-      float* o = part + (int64_t)blockIdx.x * 2 * cols;
-      for (int c = threadIdx.x; c < 2 * cols; c += blockDim.x) o[c] = s_part[c];
+      cta_sums<V, N>(dw, db, s_part, cols, tpr, R.at, part);
     } else {
       float* o = part + (int64_t)blockIdx.x * 2 * cols;
 #pragma unroll
@@ -295,26 +303,222 @@ __global__ void __launch_bounds__(CTA ? kCtaThreads : kThreads)
   }
 }
 
-// dw and db: the CTAs' sums added in order, 32 columns a CTA, eight threads a
-// column.
+// ---------------------------------------------------------------------------
+// Forward, many rows that lie one behind the other: each warp has a ring of
+// shared-memory stages that bulk copies fill, a stage the rows that the warp works on
+// at once. What is on its way takes no registers then: 131072 x 640 fp16 60 us (5.6
+// TB/s), 74 with only the next row in registers; 409600 x 320 bf16 104 and 106.
+constexpr int kRingWarps = 8;
+constexpr int kRingStages = 8;            // at most
+constexpr size_t kRingBytes = 108 << 10;  // of a CTA, two to an SM
+
 template <typename T>
-__global__ void __launch_bounds__(256) k_norm_sums(const float* __restrict__ part, int parts, int cols, T* dw, T* db) {
-  __shared__ float s[8][33];
+struct Ring {
+  const T* x;          // the next stage's rows
+  unsigned char* mem;  // this warp's stages
+  uint64_t* full;
+  int64_t n, next, hop;  // rows that count; the next stage's first; values from a stage's first row to the next one's
+  int rows, step, cols, stages, bytes, fill, take;
+  uint32_t parity;
+  bool bad;
+
+  __device__ __forceinline__ Ring(const T* x_, unsigned char* smem, uint64_t (*bars)[kRingStages], int64_t n_, int cols_, int tpr,
+                                  int stages_)
+      : n(n_), rows(32 / tpr), cols(cols_), stages(stages_), fill(0), take(0), parity(0), bad(false) {
+    const int warp = threadIdx.x >> 5;
+    bytes = rows * cols * (int)sizeof(T);
+    mem = smem + (size_t)warp * stages * bytes;
+    full = bars[warp];
+    next = ((int64_t)blockIdx.x * kRingWarps + warp) * rows;
+    step = (int)gridDim.x * kRingWarps * rows;
+    hop = (int64_t)step * cols;
+    x = x_ + next * cols;
+    if ((threadIdx.x & 31) == 0) {
+      for (int s = 0; s < stages; ++s) mbar_init(full + s, 1);
+      fence_barrier_init();
+      for (int s = 0; s < stages; ++s) request();
+    }
+    __syncwarp();
+  }
+  __device__ __forceinline__ void request() {  // one lane: the next stage's copy
+    if (next < n) {
+      const uint32_t size = next + rows <= n ? (uint32_t)bytes : (uint32_t)((n - next) * cols) * sizeof(T);
+      mbar_arrive_expect_tx(full + fill, size);
+      bulk_g2s(mem + (size_t)fill * bytes, x, size, full + fill);
+    }
+    next += step;
+    x += hop;
+    if (++fill == stages) fill = 0;
+  }
+  // The stage in turn, and that the warp is done with it.
+  __device__ __forceinline__ const T* open(int32_t* status) {
+    wait_or_bad(full + take, parity, bad, status);
+    __syncwarp();
+    return reinterpret_cast<const T*>(mem + (size_t)take * bytes);
+  }
+  __device__ __forceinline__ void close() {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) request();
+    if (++take == stages) {
+      take = 0;
+      parity ^= 1;
+    }
+  }
+};
+
+template <typename T, int N>
+__global__ void __launch_bounds__(kRingWarps * 32, 2)
+    k_norm_ring(const T* x, const T* __restrict__ w, const T* __restrict__ b, float eps, T* y, int64_t ys, float* mean, float* rstd,
+                int64_t rows, int cols, int tpr, const int32_t* count, int64_t per, int stages, int32_t* status) {
+  constexpr int V = Elem<T>::kVec;
+  using P = Piece<T, V>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ __align__(8) uint64_t bars[kRingWarps][kRingStages];
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = counted(rows, count, per);
+  Ring<T> ring(x, smem, bars, n, cols, tpr, stages);
+  const Rows<false> R(tpr);
+  RowSum<false> sum(nullptr, tpr);
+  typename P::Raw wv[N], bv[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (R.at + i * tpr) * V;
+    wv[i] = w && c < cols ? P::load(w + c) : P::zero();
+    bv[i] = b && c < cols ? P::load(b + c) : P::zero();
+  }
+  const float inv = 1.f / (float)cols;
+  int64_t r = R.first;
+  for (int64_t lead = R.lead; lead < n; lead += R.step, r += R.step) {
+    float v[N * V], s[2] = {};
+    const T* in = ring.open(status) + (int)(r - lead) * cols;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (R.at + i * tpr) * V;
+      P::open(r < n && c < cols ? P::load(in + c) : P::zero(), v + i * V);
+    }
+    ring.close();
+#pragma unroll
+    for (int q = 0; q < N * V; ++q) s[q & 1] += v[q];
+    const float mu = sum(s[0] + s[1]) * inv;
+    s[0] = s[1] = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if ((R.at + i * tpr) * V < cols) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const int q = i * V + k;
+          v[q] -= mu;
+          s[q & 1] = fmaf(v[q], v[q], s[q & 1]);
+        }
+      }
+    const float rs = ring.bad ? __int_as_float(0x7fffffff) : rsqrtf(sum(s[0] + s[1]) * inv + eps);
+    if (r < n) {
+      T* o = y + r * ys;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = (R.at + i * tpr) * V;
+        if (c < cols) {
+          float f[V], wf[V], bf[V];
+          P::open(wv[i], wf);
+          P::open(bv[i], bf);
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            const float xh = v[i * V + k] * rs;
+            f[k] = w ? fmaf(xh, wf[k], bf[k]) : xh + bf[k];
+          }
+          P::store(o + c, f);
+        }
+      }
+      if (mean && R.at == 0) {
+        mean[r] = mu;
+        rstd[r] = rs;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dw and db of many rows on their own: a lane has a 16-byte piece of the columns,
+// a warp 32 of them over its rows, the warps of a CTA are added in order. With the sums
+// in the kernel of dx their registers leave eight warps to an SM: 131072 x 640 fp16 172 us
+// together; apart what both read is read twice.
+constexpr int kColWarps = 8;
+template <typename T>
+__global__ void __launch_bounds__(kColWarps * 32) k_norm_cols(const T* dy, int64_t dys, const T* x, int64_t xs,
+                                                             const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                             int64_t rows, int cols, const int32_t* count, int64_t per,
+                                                             float* __restrict__ part) {
+  constexpr int V = Elem<T>::kVec, U = 4;  // rows at once
+  using P = Piece<T, V>;
+  __shared__ float s_sum[2][32 * V];
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = counted(rows, count, per);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * V;
+  const bool there = c < cols;
+  float dw[V] = {}, db[V] = {};
+  const int64_t step = (int64_t)gridDim.y * kColWarps * U;
+  for (int64_t r0 = ((int64_t)blockIdx.y * kColWarps + warp) * U; r0 < n; r0 += step) {
+    typename P::Raw a[U], g[U];
+    float mu[U], rs[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool in = r0 + u < n;
+      a[u] = in && there ? P::load(x + (r0 + u) * xs + c) : P::zero();
+      g[u] = in && there ? P::load(dy + (r0 + u) * dys + c) : P::zero();
+      mu[u] = in ? mean[r0 + u] : 0.f;
+      rs[u] = in ? rstd[r0 + u] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float xf[V], gf[V];
+      P::open(a[u], xf);
+      P::open(g[u], gf);
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        dw[k] = fmaf(gf[k], (xf[k] - mu[u]) * rs[u], dw[k]);
+        db[k] += gf[k];
+      }
+    }
+  }
+  for (int t = 0; t < kColWarps; ++t) {
+    if (warp == t)
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        s_sum[0][k * 32 + lane] = dw[k] + (t ? s_sum[0][k * 32 + lane] : 0.f);
+        s_sum[1][k * 32 + lane] = db[k] + (t ? s_sum[1][k * 32 + lane] : 0.f);
+      }
+    __syncthreads();
+  }
+  if (warp < 2 && there) {
+    float* o = part + (int64_t)blockIdx.y * 2 * cols + warp * cols + c;
+#pragma unroll
+    for (int k = 0; k < V; ++k) o[k] = s_sum[warp][k * 32 + lane];
+  }
+}
+
+// dw and db: the CTAs' sums added in order, 32 columns a CTA, 32 threads a column
+// (a sum is a chain of loads from L2: 608 rows of 640 columns took 14 us with eight).
+constexpr int kSumGroups = 32;
+template <typename T>
+__global__ void __launch_bounds__(32 * kSumGroups) k_norm_sums(const float* __restrict__ part, int parts, int cols, T* dw, T* db) {
+  __shared__ float s[kSumGroups][33];
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x & 31, g = threadIdx.x >> 5;
   const int64_t c = (int64_t)blockIdx.x * 32 + lane;
   float v = 0.f;
   if (c < 2 * (int64_t)cols) {
-    const int lo = (int)((int64_t)parts * g / 8), hi = (int)((int64_t)parts * (g + 1) / 8);
-#pragma unroll 4
+    const int lo = parts * g / kSumGroups, hi = parts * (g + 1) / kSumGroups;
+#pragma unroll 8
     for (int p = lo; p < hi; ++p) v += __ldcg(part + (int64_t)p * 2 * cols + c);
   }
   s[g][lane] = v;
   __syncthreads();
   if (g == 0 && c < 2 * (int64_t)cols) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) v += s[i][lane];
+    for (int i = 1; i < kSumGroups; ++i) v += s[i][lane];
     T* o = c < cols ? dw : db;
     if (o) o[c < cols ? c : c - cols] = Elem<T>::put(v);
   }
@@ -451,7 +655,7 @@ cudaError_t backward(const NormArgs& a, const Form& f, int* parts, cudaStream_t 
   else {
   const int64_t per_cta = CTA ? 1 : kThreads / f.tpr;
   const int64_t want = (a.rows + per_cta - 1) / per_cta;
-  const int most = CTA ? 152 * (f.tpr > 256 ? 1 : 2) : kMaxParts;
+  const int most = CTA && f.tpr > 256 ? kMaxParts / 2 : kMaxParts;
   const int grid = (int)(want < most ? want : most);
   *parts = grid;
   const size_t smem = CTA ? 0 : (size_t)2 * a.cols * sizeof(float);
@@ -464,6 +668,23 @@ cudaError_t backward(const NormArgs& a, const Form& f, int* parts, cudaStream_t 
   }
 }
 
+template <typename T, int N>
+cudaError_t ring(const NormArgs& a, const Form& f, cudaStream_t st) {
+  const size_t stage = (size_t)kRingWarps * (32 / f.tpr) * a.cols * sizeof(T), fit = kRingBytes / stage;
+  const int stages = fit < kRingStages ? (int)fit : kRingStages;
+  static SmemGranted granted;
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_norm_ring<T, N>), stages * stage, granted);
+  if (e != cudaSuccess) return e;
+  return launch_ex(k_norm_ring<T, N>, dim3(152 * 2), dim3(kRingWarps * 32), stages * stage, st, 0, (const T*)a.x, (const T*)a.w,
+                   (const T*)a.b, a.eps, (T*)a.y, a.ys, a.mean, a.rstd, a.rows, a.cols, f.tpr, a.count, a.per, stages, a.status);
+}
+// Rings fill where every warp has two stages and more; from there on dw and db
+// are worth a pass of their own.
+template <typename T>
+bool many_rows(const NormArgs& a, const Form& f) {
+  return f.vec && !f.cta && a.rows * f.tpr >= (int64_t)2 * 32 * 152 * 2 * kRingWarps;
+}
+
 template <typename T>
 cudaError_t run(const NormArgs& a, bool back, cudaStream_t st) {
   constexpr int V = Elem<T>::kVec;
@@ -472,7 +693,28 @@ cudaError_t run(const NormArgs& a, bool back, cudaStream_t st) {
   const Form f = form_of(a.cols, V, aligned, back && V == 8 ? 4 : 8);
   int parts = 0;
   cudaError_t e = cudaSuccess;
-#define PA_NORM_CASE(VV, NN, CC) e = back ? backward<T, VV, NN, CC>(a, f, &parts, st) : forward<T, VV, NN, CC>(a, f, st)
+  if (!back && many_rows<T>(a, f) && a.xs == a.cols) {
+    switch (f.n) {
+      case 1: return ring<T, 1>(a, f, st);
+      case 2: return ring<T, 2>(a, f, st);
+      case 3: return ring<T, 3>(a, f, st);
+      case 4: return ring<T, 4>(a, f, st);
+      case 5: return ring<T, 5>(a, f, st);
+      default: break;
+    }
+  }
+  NormArgs own = a;
+  if (back && a.part && many_rows<T>(a, f)) {  // before dx, which may go over dy or x
+    const int gx = (a.cols / V + 31) / 32;
+    parts = kMaxParts / gx;
+    if (parts < 1) parts = 1;
+    e = launch_ex(k_norm_cols<T>, dim3(gx, parts), dim3(kColWarps * 32), 0, st, 0, (const T*)a.dy, a.dys, (const T*)a.x, a.xs,
+                  (const float*)a.mean, (const float*)a.rstd, a.rows, a.cols, a.count, a.per, a.part);
+    if (e != cudaSuccess) return e;
+    own.part = nullptr;
+  }
+  int used = 0;
+#define PA_NORM_CASE(VV, NN, CC) e = back ? backward<T, VV, NN, CC>(own, f, &used, st) : forward<T, VV, NN, CC>(a, f, st)
   if (f.n == 0) {
     const dim3 grid((unsigned)(a.rows < 304 ? a.rows : 304));
     if (!back)
@@ -506,8 +748,9 @@ cudaError_t run(const NormArgs& a, bool back, cudaStream_t st) {
     PA_NORM_CASE(1, 8, false);
   }
 #undef PA_NORM_CASE
+  if (own.part && f.n != 0) parts = used;
   if (e != cudaSuccess || !back || !a.part) return e;
-  return launch_ex(k_norm_sums<T>, dim3((unsigned)((2 * (int64_t)a.cols + 31) / 32)), dim3(256), 0, st, 0,
+  return launch_ex(k_norm_sums<T>, dim3((unsigned)((2 * (int64_t)a.cols + 31) / 32)), dim3(32 * kSumGroups), 0, st, 0,
                    (const float*)a.part, parts, a.cols, (T*)a.dw, (T*)a.db);
 }
 

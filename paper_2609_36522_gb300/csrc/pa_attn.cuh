@@ -7,6 +7,7 @@
 #include "pa_bulk.cuh"
 #include "pa_layers.h"
 #include "pa_tcgen05.cuh"
+#include "pa_wait.cuh"
 
 namespace pa {
 
@@ -42,29 +43,6 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// Two fp32 values in one instruction.
-struct F2 {
-  uint64_t v;
-  __device__ __forceinline__ F2() {}
-  __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-  __device__ __forceinline__ F2(uint32_t a, uint32_t b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b)); }
-  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-};
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ F2 add2(F2 a, F2 b) {
-  F2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -142,20 +120,6 @@ __device__ __forceinline__ void mma_over_d(uint32_t d, uint64_t a, int ra, uint6
 }
 __device__ __forceinline__ void mma_over_rows(uint32_t d, uint32_t a, uint64_t b, int sw, int n, uint32_t idesc, bool add) {
   for (int k = 0; k < n; ++k, a += 8, b += (uint32_t)sw) tc_mma_f16_ta(d, a, b, idesc, add || k > 0 ? 1u : 0u);
-}
-
-// Bounded wait (about a second); after a failure a thread no longer waits, runs
-// on with accesses in bounds, and the call's results are not valid.
-__device__ __forceinline__ void wait_or_bad(uint64_t* bar, uint32_t parity, bool& bad, int32_t* status) {
-  if (bad || mbar_test(bar, parity)) return;
-  const long long t0 = clock64();
-  while (!mbar_try(bar, parity)) {
-    if (clock64() - t0 > 2000000000ll) {
-      bad = true;
-      atomicCAS(status, 0, kDevTimeout);
-      return;
-    }
-  }
 }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {

@@ -131,7 +131,7 @@ pa_status attn_call(const char* where, const pa_attention_t* t, bool back, void*
   if (s != PA_OK) return s;
   if (rows == 0 && (!back || states == 0)) return PA_OK;
   a.ws = static_cast<unsigned char*>(ws);
-  cudaError_t e = pa::attn_status(&a.status);
+  cudaError_t e = pa::layers_status(&a.status);
   if (e == cudaSuccess) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     e = back ? pa::launch_attn_backward(a, st) : pa::launch_attn(a, st);
@@ -167,7 +167,9 @@ pa_status pa_layer_norm(int dtype, int64_t rows, int cols, const void* x, int64_
   if (!mean != !rstd) return arg(where, "mean and rstd go together");
   if (rows == 0) return PA_OK;
   if (!x || !y) return arg(where, "x or y is NULL");
-  return done(where, pa::launch_norm(a, static_cast<cudaStream_t>(stream)));
+  cudaError_t e = pa::layers_status(&a.status);
+  if (e == cudaSuccess) e = pa::launch_norm(a, static_cast<cudaStream_t>(stream));
+  return done(where, e);
 }
 
 size_t pa_layer_norm_backward_workspace_bytes(int64_t rows, int cols) {
@@ -213,7 +215,9 @@ pa_status pa_layer_norm_backward(int dtype, int64_t rows, int cols, const void* 
     }
   }
   if (rows == 0) return PA_OK;
-  return done(where, pa::launch_norm_backward(a, st));
+  cudaError_t e = pa::layers_status(&a.status);
+  if (e == cudaSuccess) e = pa::launch_norm_backward(a, st);
+  return done(where, e);
 }
 
 size_t pa_attention_workspace_bytes(const pa_attention_t* t, int backward) {
@@ -230,11 +234,11 @@ pa_status pa_attention_backward(const pa_attention_t* a, void* workspace_dev, si
   return attn_call("pa_attention_backward", a, true, workspace_dev, workspace_bytes, stream);
 }
 
-pa_status pa_attention_check(void* stream) {
-  const char* where = "pa_attention_check";
+pa_status pa_layers_check(void* stream) {
+  const char* where = "pa_layers_check";
   int32_t *word = nullptr, got = 0;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = pa::attn_status(&word);
+  cudaError_t e = pa::layers_status(&word);
   if (e == cudaSuccess) e = cudaMemcpyAsync(&got, word, sizeof got, cudaMemcpyDeviceToHost, st);
   if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, sizeof got, st);
   if (e == cudaSuccess) e = cudaStreamSynchronize(st);

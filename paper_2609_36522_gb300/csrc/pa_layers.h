@@ -78,6 +78,30 @@ struct Elem<__nv_bfloat16> {
   }
 };
 
+// Two fp32 values in one instruction.
+struct F2 {
+  uint64_t v;
+  __device__ __forceinline__ F2() {}
+  __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ F2(uint32_t a, uint32_t b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b)); }
+  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
 // ---- layer norm -------------------------------------------------------------
 struct NormArgs {
   int dtype;
@@ -92,6 +116,7 @@ struct NormArgs {
   float *mean, *rstd;     // written forward (NULL: not kept), read backward
   const int32_t* count;   // device: the first *count groups of `per` rows count (NULL: all rows)
   int64_t per;
+  int32_t* status;        // device: first failure
   // backward
   const void* dy;
   int64_t dys;
@@ -134,7 +159,7 @@ size_t attn_workspace(const AttnArgs& a);
 size_t attn_backward_workspace(const AttnArgs& a);
 cudaError_t launch_attn(const AttnArgs& a, cudaStream_t st);
 cudaError_t launch_attn_backward(const AttnArgs& a, cudaStream_t st);
-// The device's status word (k_attn.cu).
-cudaError_t attn_status(int32_t** out);
+// The device's status word of the layer calls (k_attn.cu).
+cudaError_t layers_status(int32_t** out);
 
 }  // namespace pa

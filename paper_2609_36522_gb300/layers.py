@@ -308,8 +308,8 @@ def cross_attention_workspace_bytes(q, k, mask=False, backward=False):
 
 
 def check(stream=None):
-    """Wait for ``stream`` (default: the current one) and raise PaError if an
-    attention call met a source index out of range or a wait that ran out."""
+    """Wait for ``stream`` (default: the current one) and raise PaError if a call
+    of this module met a source index out of range or a wait that ran out."""
     if stream is None:
         stream = torch.cuda.current_stream()
-    abi.pa_attention_check(stream.cuda_stream)
+    abi.pa_layers_check(stream.cuda_stream)
