@@ -2,6 +2,8 @@
 // the states of the item's source,
 //   s_j = scale q . k_j,  p_j = exp(s_j - max s),  o = sum p_j v_j / sum p_j,
 // over the source's keys that count; lse = max s + ln sum p_j.
+#include <type_traits>
+
 #include "pa_attn.cuh"
 
 namespace pa {
@@ -46,18 +48,21 @@ __global__ void __launch_bounds__(kListThreads) k_attn_keys(const uint8_t* __res
 
 // ---------------------------------------------------------------------------
 // CUDA cores: RT rows of one key head per CTA. The lanes of a group of `gs`
-// hold eight values each of a key; a warp works on 32 / gs keys at a time, four
-// times that at once, every group with a running maximum and sum of its own;
-// groups and warps are joined at the end.
+// hold eight values each of a key; a warp works on 32 / gs keys at a time, twice
+// that at once with the next ones on their way, every group with a running maximum
+// and sum of its own; groups and warps are joined at the end. Bound by the reads of
+// the keys and values: what counts is bytes in flight, so registers are kept to two
+// CTAs an SM.
 constexpr int kRowWarps = 8;
-constexpr int kRowKeys = 4;  // keys in flight per group
+constexpr int kRowKeys = 2;  // keys of a group at once
 
-template <typename T, int RT>
-__global__ void __launch_bounds__(kRowWarps * 32) k_attn_rows(AttnArgs a, Keys keys, int gs, int chunks, int splits,
+template <typename T, int RT, int gs>
+__global__ void __launch_bounds__(kRowWarps * 32, 2) k_attn_rows(AttnArgs a, Keys keys, int chunks, int splits,
                                                              float* __restrict__ po, float* __restrict__ pl) {
   extern __shared__ float smem[];  // [warp][RT][D], then [warp][RT] maxima and sums
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int at = lane & (gs - 1), kpw = 32 / gs, R = a.H / a.J;
+  constexpr int kpw = 32 / gs;
+  const int at = lane & (gs - 1), R = a.H / a.J;
   pdl_wait();
   pdl_trigger();
   int64_t b = blockIdx.x;
@@ -89,30 +94,54 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_attn_rows(AttnArgs a, Keys k
   }
   const T* kp = (const T*)a.k + (int64_t)max(g, 0) * a.ks.item + j * a.ks.head + at * 8;
   const T* vp = (const T*)a.v + (int64_t)max(g, 0) * a.vs.item + j * a.vs.head + at * 8;
-  for (int k0 = lo + warp * kpw * kRowKeys; k0 < hi; k0 += kRowWarps * kpw * kRowKeys) {
-    uint4 ku[kRowKeys], vu[kRowKeys];
+  uint4 ku[kRowKeys], vu[kRowKeys];
+  constexpr int stride = kRowWarps * kpw * kRowKeys;
+  int next = lo + warp * kpw * kRowKeys + lane / gs;  // this group's next key
+  const T *kq = kp + next * a.ks.token, *vq = vp + next * a.vs.token;
+  const int64_t kstep = kpw * a.ks.token, vstep = kpw * a.vs.token;
+  auto fetch = [&] {
+#pragma unroll
+    for (int u = 0; u < kRowKeys; ++u) {
+      const int i = next + u * kpw;
+      ku[u] = vu[u] = make_uint4(0, 0, 0, 0);
+      if (i < hi && col) {
+        if (keys.list) {
+          const int64_t key = keys.at(g, i);
+          ku[u] = *reinterpret_cast<const uint4*>(kp + key * a.ks.token);
+          vu[u] = *reinterpret_cast<const uint4*>(vp + key * a.vs.token);
+        } else {
+          ku[u] = *reinterpret_cast<const uint4*>(kq + u * kstep);
+          vu[u] = *reinterpret_cast<const uint4*>(vq + u * vstep);
+        }
+      }
+    }
+    next += stride;
+    kq += stride / kpw * kstep;
+    vq += stride / kpw * vstep;
+  };
+  int k0 = lo + warp * kpw * kRowKeys;
+  fetch();
+  for (; k0 < hi; k0 += stride) {
+    uint4 kc[kRowKeys], vc[kRowKeys];
     bool in[kRowKeys];
 #pragma unroll
     for (int u = 0; u < kRowKeys; ++u) {
-      const int i = k0 + u * kpw + lane / gs;
-      in[u] = i < hi;
-      ku[u] = vu[u] = make_uint4(0, 0, 0, 0);
-      if (in[u] && col) {
-        const int64_t key = keys.at(g, i);
-        ku[u] = *reinterpret_cast<const uint4*>(kp + key * a.ks.token);
-        vu[u] = *reinterpret_cast<const uint4*>(vp + key * a.vs.token);
-      }
+      kc[u] = ku[u];
+      vc[u] = vu[u];
+      in[u] = k0 + u * kpw + lane / gs < hi;
     }
+    fetch();
     float s[kRowKeys][RT];
 #pragma unroll
     for (int u = 0; u < kRowKeys; ++u) {
       float kf[8];
-      Elem<T>::open(ku[u], kf);
+      Elem<T>::open(kc[u], kf);
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
         float d = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) d = fmaf(q[r][i], kf[i], d);
+#pragma unroll
         for (int o = gs >> 1; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
         s[u][r] = in[u] ? d : -INFINITY;
       }
@@ -122,11 +151,14 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_attn_rows(AttnArgs a, Keys k
       float mx = m[r];
 #pragma unroll
       for (int u = 0; u < kRowKeys; ++u) mx = fmaxf(mx, s[u][r]);
-      const float base = mx == -INFINITY ? 0.f : mx, f = ex2(m[r] - base);
-      m[r] = mx;
-      l[r] *= f;
+      if (__any_sync(0xffffffffu, mx > m[r])) {  // seldom after the first keys
+        const float f = m[r] == -INFINITY ? 0.f : ex2(m[r] - mx);
+        m[r] = mx;
+        l[r] *= f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[r][i] *= f;
+        for (int i = 0; i < 8; ++i) acc[r][i] *= f;
+      }
+      const float base = m[r] == -INFINITY ? 0.f : m[r];
 #pragma unroll
       for (int u = 0; u < kRowKeys; ++u) {
         s[u][r] = ex2(s[u][r] - base);
@@ -136,7 +168,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_attn_rows(AttnArgs a, Keys k
 #pragma unroll
     for (int u = 0; u < kRowKeys; ++u) {
       float vf[8];
-      Elem<T>::open(vu[u], vf);
+      Elem<T>::open(vc[u], vf);
 #pragma unroll
       for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -146,6 +178,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_attn_rows(AttnArgs a, Keys k
   // the groups of a warp
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
+#pragma unroll
     for (int o = gs; o < 32; o <<= 1) {
       const float mo = __shfl_xor_sync(0xffffffffu, m[r], o), mx = fmaxf(m[r], mo), base = mx == -INFINITY ? 0.f : mx;
       const float f = ex2(m[r] - base), fo = ex2(mo - base);
@@ -257,7 +290,7 @@ Plan plan(const AttnArgs& a) {
   p.chunks = (int)((rows + p.rt - 1) / p.rt);
   for (p.gs = 1; p.gs * 8 < a.D;) p.gs <<= 1;
   const int64_t ctas = (int64_t)a.N * a.J * p.chunks;
-  const int64_t want = (608 + ctas - 1) / ctas, most = (a.K + 255) / 256;
+  const int64_t want = (3 * 608 + ctas - 1) / ctas, most = (a.K + 255) / 256;
   p.splits = (int)(want < most ? want : most);
   if (p.splits < 1) p.splits = 1;
   p.tc = rows > kRowsMost;
@@ -294,8 +327,25 @@ cudaError_t run(const AttnArgs& a, cudaStream_t st) {
   float* pl = reinterpret_cast<float*>(a.ws + p.pl);
   const dim3 grid((unsigned)((int64_t)a.N * a.J * p.chunks), p.splits);
   const size_t smem = (size_t)kRowWarps * p.rt * (a.D + 2) * 4;
-  e = p.tc ? launch_attn_tc(a, keys, po, pl, st) : launch_ex(p.rt == 1 ? k_attn_rows<T, 1> : k_attn_rows<T, 4>, grid, dim3(kRowWarps * 32), smem, st, 0, a, keys, p.gs,
-                p.chunks, p.splits, po, pl);
+  if (p.tc) {
+    e = launch_attn_tc(a, keys, po, pl, st);
+  } else {
+    const auto go = [&](auto kern) {
+      return launch_ex(kern, grid, dim3(kRowWarps * 32), smem, st, 0, a, keys, p.chunks, p.splits, po, pl);
+    };
+    const auto rows = [&](auto g) {
+      constexpr int gs = decltype(g)::value;
+      return p.rt == 1 ? go(k_attn_rows<T, 1, gs>) : go(k_attn_rows<T, 4, gs>);
+    };
+    switch (p.gs) {
+      case 1: e = rows(std::integral_constant<int, 1>{}); break;
+      case 2: e = rows(std::integral_constant<int, 2>{}); break;
+      case 4: e = rows(std::integral_constant<int, 4>{}); break;
+      case 8: e = rows(std::integral_constant<int, 8>{}); break;
+      case 16: e = rows(std::integral_constant<int, 16>{}); break;
+      default: e = rows(std::integral_constant<int, 32>{}); break;
+    }
+  }
   if (e != cudaSuccess || p.splits == 1) return e;
   const int64_t pieces = (int64_t)a.N * a.Q * a.H * (a.D / 8), ctas = (pieces + 255) / 256;
   return launch_ex(k_attn_join<T>, dim3((unsigned)(ctas < 1216 ? ctas : 1216)), dim3(256), 0, st, 0, a, p.splits,
