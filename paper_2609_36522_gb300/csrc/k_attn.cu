@@ -12,38 +12,73 @@ namespace {
 __device__ int32_t g_status;
 
 // ---------------------------------------------------------------------------
-// The keys of each source that count, in order; a CTA per source. pos (may be
-// NULL): each key's place among them, -1 for the others.
-constexpr int kListThreads = 256;
-__global__ void __launch_bounds__(kListThreads) k_attn_keys(const uint8_t* __restrict__ mask, int64_t stride,
-                                                           const int32_t* __restrict__ len, int K, int32_t* __restrict__ n,
-                                                           int32_t* __restrict__ list, int32_t* __restrict__ pos) {
-  __shared__ int s_n[kListThreads / 32];
+// Lists, a CTA per source. With a mask (n): the keys of the source that count, in
+// order, and, for the backward pass (pos), each key's place among them, -1 for the
+// others. For the backward pass (first): the source's items in order, behind those of
+// the sources before it; first[2 g], first[2 g + 1] bound them.
+constexpr int kListThreads = 256, kListWarps = kListThreads / 32;
+
+// How many of the CTA's threads before this one are in, and how many there are; every thread.
+__device__ __forceinline__ int before_me(bool in, int* s_n, int& all) {
+  const unsigned b = __ballot_sync(0xffffffffu, in);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (lane == 0) s_n[warp] = __popc(b);
+  __syncthreads();
+  int n = __popc(b & ((1u << lane) - 1));
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kListWarps; ++w) {
+    if (w < warp) n += s_n[w];
+    all += s_n[w];
+  }
+  __syncthreads();
+  return n;
+}
+
+__global__ void __launch_bounds__(kListThreads) k_attn_lists(AttnArgs a, int32_t* __restrict__ n, int32_t* __restrict__ list,
+                                                            int32_t* __restrict__ pos, int32_t* __restrict__ first,
+                                                            int32_t* __restrict__ order) {
+  __shared__ int s_n[kListWarps];
   pdl_wait();
   pdl_trigger();
-  const int g = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int end = len ? min(max(len[g], 0), K) : K;
-  const uint8_t* m = mask + g * stride;
-  int base = 0;
-  for (int k0 = 0; k0 < (pos ? K : end); k0 += kListThreads) {
-    const int k = k0 + threadIdx.x;
-    const bool in = k < end && m[k] != 0;
-    const unsigned b = __ballot_sync(0xffffffffu, in);
-    if (lane == 0) s_n[warp] = __popc(b);
-    __syncthreads();
-    int before = base;
-#pragma unroll
-    for (int w = 0; w < kListThreads / 32; ++w) {
-      const int c = s_n[w];
-      if (w < warp) before += c;
-      base += c;
+  const int g = blockIdx.x;
+  if (n) {
+    const int end = a.len ? min(max(a.len[g], 0), a.K) : a.K;
+    const uint8_t* m = a.mask + g * a.mask_stride;
+    int base = 0, all;
+    for (int k0 = 0; k0 < (pos ? a.K : end); k0 += kListThreads) {
+      const int k = k0 + threadIdx.x;
+      const bool in = k < end && m[k] != 0;
+      const int at = base + before_me(in, s_n, all);
+      if (in) list[(int64_t)g * a.K + at] = k;
+      if (pos && k < a.K) pos[(int64_t)g * a.K + k] = in ? at : -1;
+      base += all;
     }
-    before += __popc(b & ((1u << lane) - 1));
-    if (in) list[(int64_t)g * K + before] = k;
-    if (pos && k < K) pos[(int64_t)g * K + k] = in ? before : -1;
-    __syncthreads();
+    if (threadIdx.x == 0) n[g] = base;
   }
-  if (threadIdx.x == 0) n[g] = base;
+  if (first) {
+    const int items = items_of(a.count, a.N);
+    int less = 0, base = 0, all;
+    for (int i = threadIdx.x; i < items; i += kListThreads) {
+      const int s = a.src[i * a.src_stride];
+      less += s >= 0 && s < g;
+    }
+    less = __reduce_add_sync(0xffffffffu, less);
+    if ((threadIdx.x & 31) == 0) s_n[threadIdx.x >> 5] = less;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kListWarps; ++w) base += s_n[w];
+    __syncthreads();
+    if (threadIdx.x == 0) first[2 * g] = base;
+    for (int i0 = 0; i0 < items; i0 += kListThreads) {
+      const int i = i0 + threadIdx.x;
+      const bool in = i < items && a.src[i * a.src_stride] == g;
+      const int at = base + before_me(in, s_n, all);
+      if (in) order[at] = i;
+      base += all;
+    }
+    if (threadIdx.x == 0) first[2 * g + 1] = base;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -273,9 +308,10 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a, int splits, const
   }
 }
 
-// Up to this many query rows of an item and key head the CUDA cores take them:
-// a tile of the tensor-core kernel has 128.
-constexpr int kRowsMost = 16;
+// Up to this many query rows of an item and key head the CUDA cores take them, all
+// at once; a tile of the tensor-core kernel has 128, empty or not (four rows against
+// up to 4096 keys of 64: 99 us here, 125 there, and here more rows read the keys again).
+constexpr int kRowsMost = 4;
 
 // How a call is split, and its workspace.
 struct Plan {
@@ -315,10 +351,10 @@ cudaError_t run(const AttnArgs& a, cudaStream_t st) {
   const Plan p = plan(a);
   Keys keys{a.K, a.len, nullptr, nullptr};
   cudaError_t e = cudaSuccess;
-  if (a.mask) {
+  if (a.mask && a.G > 0) {
     int32_t* n = reinterpret_cast<int32_t*>(a.ws + p.n);
     int32_t* list = reinterpret_cast<int32_t*>(a.ws + p.list);
-    e = launch_attn_keys(a, n, list, nullptr, st);
+    e = launch_attn_lists(a, n, list, nullptr, nullptr, nullptr, st);
     if (e != cudaSuccess) return e;
     keys.n = n;
     keys.list = list;
@@ -354,8 +390,9 @@ cudaError_t run(const AttnArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_attn_keys(const AttnArgs& a, int32_t* n, int32_t* list, int32_t* pos, cudaStream_t st) {
-  return launch_ex(k_attn_keys, dim3(a.G), dim3(kListThreads), 0, st, 0, a.mask, a.mask_stride, a.len, a.K, n, list, pos);
+cudaError_t launch_attn_lists(const AttnArgs& a, int32_t* n, int32_t* list, int32_t* pos, int32_t* first, int32_t* order,
+                              cudaStream_t st) {
+  return launch_ex(k_attn_lists, dim3(a.G), dim3(kListThreads), 0, st, 0, a, n, list, pos, first, order);
 }
 
 size_t attn_workspace(const AttnArgs& a) { return plan(a).total; }

@@ -549,11 +549,12 @@ cudaError_t go(const AttnArgs& a, const Keys& keys, const TcPlan& p, float* po, 
   Maps m;
   TcShape s = p.sh;
   const int R = a.H / a.J, sw = s.box.sw, w = sw / 2;
-  s.q_bulk = 128 % R == 0 &&
+  const bool rows = worth_a_map((int64_t)a.N * a.Q * a.H, a.D), states = worth_a_map((int64_t)a.G * a.K * a.J, a.D);
+  s.q_bulk = rows && 128 % R == 0 &&
              make_map(&m.q, a.dtype, a.q, a.D, a.H, a.Q, a.N, a.qs.head, a.qs.token, a.qs.item, w, R, 128 / R, sw);
-  s.k_bulk = !keys.list && make_map(&m.k, a.dtype, a.k, a.D, a.J, a.K, a.G, a.ks.head, a.ks.token, a.ks.item, w, 1, s.kt, sw) &&
+  s.k_bulk = (rows || states) && !keys.list && make_map(&m.k, a.dtype, a.k, a.D, a.J, a.K, a.G, a.ks.head, a.ks.token, a.ks.item, w, 1, s.kt, sw) &&
              make_map(&m.v, a.dtype, a.v, a.D, a.J, a.K, a.G, a.vs.head, a.vs.token, a.vs.item, w, 1, s.kt, sw);
-  s.o_bulk = s.o_bulk && make_map(&m.out, a.dtype, a.o, a.D, a.H, a.Q, a.N, a.os.head, a.os.token, a.os.item, s.obox.wide, R,
+  s.o_bulk = rows && s.o_bulk && make_map(&m.out, a.dtype, a.o, a.D, a.H, a.Q, a.N, a.os.head, a.os.token, a.os.item, s.obox.wide, R,
                                   32 / R, s.obox.sw);
   return launch_ex(k_attn_tc<T, NWG, L>, dim3(p.grid), dim3(tc_threads<NWG>()), p.smem, st, 0, m, a, keys, s, po, pl);
 }

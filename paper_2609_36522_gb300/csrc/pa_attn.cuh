@@ -15,7 +15,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr int kDevBadSource = 4;  // an item's source outside [0, G): the item has no keys
 
 // Keys of a source that count, in order. With a mask a list of them is made
-// first (k_attn_keys), so that dropped keys are neither read nor multiplied:
+// first (k_attn_lists), so that dropped keys are neither read nor multiplied:
 // what lies there (infinities, NaN) cannot reach a result.
 struct Keys {
   int K;
@@ -326,7 +326,9 @@ __device__ __forceinline__ void rows_out_bulk(const CUtensorMap* map, int head, 
   }
 }
 
-// Tensor maps of a call, made on the host; use: whether the map could be made.
+// Tensor maps of a call, made on the host at about a microsecond each: only for
+// tensors of a megabyte and more, which bulk copies save that many times over.
+__host__ inline bool worth_a_map(int64_t rows, int D) { return rows * D * 2 >= (int64_t)1 << 20; }
 struct Maps {
   CUtensorMap q, k, v, out, dout;
 };
@@ -335,8 +337,9 @@ struct Maps {
 bool make_map(CUtensorMap* map, int dtype, const void* base, int D, int64_t n1, int64_t n2, int64_t n3, int64_t s1, int64_t s2,
               int64_t s3, int cols, int b1, int b2, int sw);
 
-// The list above (k_attn.cu).
-cudaError_t launch_attn_keys(const AttnArgs& a, int32_t* n, int32_t* list, int32_t* pos, cudaStream_t st);
+// Lists of keys and items (k_attn.cu); what is NULL is not made.
+cudaError_t launch_attn_lists(const AttnArgs& a, int32_t* n, int32_t* list, int32_t* pos, int32_t* first, int32_t* order,
+                              cudaStream_t st);
 // The forward pass on the tensor cores (k_attn_tc.cu); parts of the keys, 1:
 // none, else po [row][part][D] and pl [row][part] are written for the join.
 int attn_tc_splits(const AttnArgs& a);

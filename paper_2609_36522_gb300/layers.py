@@ -80,7 +80,7 @@ def _workspace(workspace, need, like):
     if need == 0:
         return None, 0, None
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+        workspace = like.new_empty(need, dtype=torch.uint8)
         return workspace.data_ptr(), need, workspace
     _device("workspace", workspace, like)
     if not workspace.is_contiguous():
@@ -151,16 +151,15 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, stats=False, out=None, mean=
     w, b = _weight("weight", weight, x), _weight("bias", bias, x)
     with _place(x, stream):
         if out is None:
-            out, ys = (torch.empty_like(x), xs) if x.is_contiguous() else (torch.empty(x.shape, dtype=x.dtype, device=x.device),
-                                                                          x.shape[-1])
+            out, ys = x.new_empty(x.shape), x.shape[-1]
         else:
             _, ys = _rows("out", out, x)
         mp = rp = None
         if stats or mean is not None or rstd is not None:
             if mean is None:
-                mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+                mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
             if rstd is None:
-                rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+                rstd = x.new_empty(x.shape[:-1], dtype=torch.float32)
             mp, rp = _stat("mean", mean, x), _stat("rstd", rstd, x)
         abi.pa_layer_norm(dtype, rows, x.shape[-1], x.data_ptr(), xs, w, b, eps, out.data_ptr(), ys, mp, rp,
                           _count(count, x), _per_item(x, rows), _raw_stream(x.get_device()))
@@ -180,12 +179,12 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, weight_grad=True, bias_g
     w, mp, rp = _weight("weight", weight, x), _stat("mean", mean, x), _stat("rstd", rstd, x)
     with _place(x, stream):
         if dx is None:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            dx = x.new_empty(x.shape)
             dxs = cols
         else:
             _, dxs = _rows("dx", dx, x)
-        dw = torch.empty(cols, dtype=x.dtype, device=x.device) if weight_grad else None
-        db = torch.empty(cols, dtype=x.dtype, device=x.device) if bias_grad else None
+        dw = x.new_empty(cols) if weight_grad else None
+        db = x.new_empty(cols) if bias_grad else None
         need = abi.pa_layer_norm_backward_workspace_bytes(rows, cols) if weight_grad or bias_grad else 0
         ws, nbytes, keep = _workspace(workspace, need, x)
         abi.pa_layer_norm_backward(dtype, rows, cols, dy.data_ptr(), dys, x.data_ptr(), xs, w, mp, rp, dx.data_ptr(), dxs,
@@ -270,10 +269,10 @@ def cross_attention(q, k, v, scale=None, source=None, lengths=None, mask=None, c
     given = _inputs(q, k, v, scale, source, lengths, mask, count)
     with _place(q, stream):
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
         op, os = _tensor("out", out, q)
         if stats and lse is None:
-            lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+            lse = q.new_empty(q.shape[:3], dtype=torch.float32)
         block = _BLOCK.pack(*given, op, *os, 0 if lse is None else _lse(lse, q), *_NO_GRADIENTS)
         ws, nbytes, keep = _workspace(workspace, abi.pa_attention_workspace_bytes(block, 0), q)
         abi.pa_attention(block, ws, nbytes, _raw_stream(q.get_device()))
@@ -289,9 +288,9 @@ def cross_attention_backward(dout, q, k, v, out, lse, scale=None, source=None, l
     (op, os), (gp, gs) = _tensor("out", out, q), _tensor("dout", dout, q)
     lp = _lse(lse, q)
     with _place(q, stream):
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-        dk = torch.empty(k.shape, dtype=q.dtype, device=q.device) if dk is None else dk
-        dv = torch.empty(v.shape, dtype=q.dtype, device=q.device) if dv is None else dv
+        dq = q.new_empty(q.shape) if dq is None else dq
+        dk = q.new_empty(k.shape) if dk is None else dk
+        dv = q.new_empty(v.shape) if dv is None else dv
         (qp, qs), (kp, ks), (vp, vs) = _tensor("dq", dq, q), _tensor("dk", dk, k), _tensor("dv", dv, v)
         block = _BLOCK.pack(*given, op, *os, lp, gp, qp, kp, vp, *gs, *qs, *ks, *vs)
         ws, nbytes, keep = _workspace(workspace, abi.pa_attention_workspace_bytes(block, 1), q)
