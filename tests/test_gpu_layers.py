@@ -101,6 +101,37 @@ def test_norm_many_rows(dtype):
     _norm_check(*_norm_inputs(20011, 72, dtype))
 
 
+@pytest.mark.parametrize("dtype,rows,cols", [("fp32", 60001, 72), ("bf16", 80003, 72), ("fp16", 20005, 320), ("bf16", 30001, 128),
+                                             ("fp32", 9001, 1000)])
+def test_norm_rows_through_rings_and_sums_of_their_own(dtype, rows, cols):
+    """As many rows as the kernels for many rows ask for, a last stage that is not full; also not one behind the
+    other, over themselves, with a device count that ends inside a stage."""
+    from paper_2609_36522_gb300 import layers
+    torch, _ = _torch()
+    x, w, b, dy = _norm_inputs(rows, cols, dtype)
+    _norm_check(x, w, b, dy)
+    y, mean, rstd = layers.layer_norm(x, w, b, stats=True)
+    dx, dw, db = layers.layer_norm_backward(dy, x, mean, rstd, w)
+    wide = torch.zeros(rows, cols + 8, dtype=x.dtype, device="cuda")
+    wide[:, :cols] = x
+    _near(layers.layer_norm(wide[:, :cols], w, b), *_norm_ref(x, w, b, dy, 1e-5)["y"], "y")
+    over = x.clone()
+    assert (layers.layer_norm(over, w, b, out=over) == y).all()
+    over = dy.clone()
+    again = layers.layer_norm_backward(over, x, mean, rstd, w, dx=over)
+    assert (over == dx).all() and (again[1] == dw).all() and (again[2] == db).all()
+    n = rows - 37
+    count = torch.tensor([n], dtype=torch.int32, device="cuda")
+    out = torch.full_like(x, 7.0)
+    layers.layer_norm(x, w, b, out=out, count=count)
+    assert (out[:n] == y[:n]).all() and (out[n:] == 7.0).all()
+    dx2, dw2, db2 = layers.layer_norm_backward(dy, x, mean, rstd, w, dx=torch.full_like(x, 7.0), count=count)
+    assert (dx2[:n] == dx[:n]).all() and (dx2[n:] == 7.0).all()
+    ref = _norm_ref(x[:n], w, b, dy[:n], 1e-5)
+    _near(dw2, *ref["dw"], "dw")
+    _near(db2, *ref["db"], "db")
+
+
 def test_norm_without_weights_and_single_gradients():
     from paper_2609_36522_gb300 import layers
     x, w, b, dy = _norm_inputs(21, 96, "bf16")
@@ -348,6 +379,22 @@ def test_attention_keys_that_do_not_count(shape, keep):
     for n, g in enumerate(kw["source"].tolist()):
         if not kept[g].any():
             assert not out[n].any() and not dq[n].any()
+
+
+# tensors of a megabyte and more go by bulk copies: whole tiles, tiles of several heads, last tiles, heads off the
+# block widths, groups of heads that no tile holds whole
+LARGE = [
+    (10, 2, 515, 77, 4, 4, 40), (6, 3, 600, 300, 4, 2, 64), (4, 2, 700, 500, 3, 3, 128), (6, 2, 1024, 64, 3, 1, 80),
+    (40, 4, 64, 100, 4, 4, 80), (30, 2, 1000, 90, 2, 2, 24), (4, 2, 520, 260, 8, 1, 160), (3, 1, 400, 333, 4, 2, 256),
+    (70, 1, 1024, 31, 1, 1, 8), (8, 8, 130, 2000, 4, 4, 96), (20, 2, 1024, 150, 2, 2, 16), (5, 2, 600, 140, 2, 2, 208),
+]
+
+
+@pytest.mark.parametrize("keep", ["all", "lengths", "mask"])
+@pytest.mark.parametrize("shape", LARGE, ids=lambda s: "x".join(map(str, s)))
+def test_attention_by_bulk_copies(shape, keep):
+    q, k, v, do, kw = _attn_inputs(*shape, "bf16" if shape[0] % 4 else "fp16", keep=keep)
+    _attn_check(q, k, v, do, kw)
 
 
 def test_attention_sources_in_any_order_and_unused():
