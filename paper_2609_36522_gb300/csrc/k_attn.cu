@@ -325,7 +325,7 @@ Plan plan(const AttnArgs& a) {
   p.rt = rows > 1 ? 4 : 1;
   p.chunks = (int)((rows + p.rt - 1) / p.rt);
   for (p.gs = 1; p.gs * 8 < a.D;) p.gs <<= 1;
-  const int64_t ctas = (int64_t)a.N * a.J * p.chunks;
+  const int64_t some = (int64_t)a.N * a.J * p.chunks, ctas = some > 0 ? some : 1;
   const int64_t want = (3 * 608 + ctas - 1) / ctas, most = (a.K + 255) / 256;
   p.splits = (int)(want < most ? want : most);
   if (p.splits < 1) p.splits = 1;

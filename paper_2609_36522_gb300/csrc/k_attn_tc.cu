@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
   constexpr int kBf16 = Elem<T>::kBf16, LT = tc_load<NWG>();
   extern __shared__ __align__(1024) unsigned char smem[];
   __shared__ __align__(8) uint64_t q_full[2][NWG], q_empty[2], k_full[kStages], k_empty[kStages], v_full[kStages],
-      v_empty[kStages], s_full[NWG][L], p_full[NWG][L], o_full[NWG];
+      v_empty[kStages], s_full[NWG][L], p_full[NWG][L], o_full[NWG][L];
   __shared__ uint32_t s_taddr;
   __shared__ Work s_work[kTable];
   __shared__ int64_t s_rows[2][128];
@@ -91,8 +91,8 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       for (int b = 0; b < L; ++b) {
         mbar_init(&s_full[g][b], 1);
         mbar_init(&p_full[g][b], 4);
+        mbar_init(&o_full[g][b], 1);
       }
-      mbar_init(&o_full[g], 1);
     }
     fence_barrier_init();
   }
@@ -160,8 +160,10 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
       float m, l;
     } pend;
     bool pending = false;
-    auto mmas_done = [&](uint32_t c) {  // the O += P V of this group's first c key tiles
-      wait_or_bad(&o_full[g], (c - 1) & 1u, bad, a.status);
+    // The O += P V of this group's first c key tiles are complete. (A barrier per place of S: the
+    // last two may both be outstanding, and one barrier's parity would take the one before for the last.)
+    auto mmas_done = [&](uint32_t c) {
+      wait_or_bad(&o_full[g][L == 1 ? 0 : (c - 1) & 1u], ((c - 1) / L) & 1u, bad, a.status);
       __syncwarp();
       tc_fence_after_sync();
     };
@@ -409,7 +411,7 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
         tc_fence_after_sync();
         if (elect_one()) {
           mma_over_rows(t0 + L * kt, t0 + b * kt, dv0 + e.st * uk, box.sw, e.n16 / 16, idesc2, !e.first);
-          tc_commit(&o_full[g]);
+          tc_commit(&o_full[g][b]);
           if (e.release) tc_commit(&v_empty[e.st]);
         }
       } else {
