@@ -455,9 +455,10 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
     const float c2 = a.scale * kLog2e;
     uint32_t par = 0;
     for (int i = s; i < tiles; i += NS) {
-      wait_or_bad(&q_full[i % sh.stages], (i / sh.stages) & 1u, bad, a.status);  // lse and delta
       wait_or_bad(&s_full[s], par, bad, a.status);
       par ^= 1;
+      // lse and delta; after S, which waited for the same phase: the next one cannot have begun
+      wait_or_bad(&q_full[i % sh.stages], (i / sh.stages) & 1u, bad, a.status);
       __syncwarp();
       tc_fence_after_sync();
       const float4* st = reinterpret_cast<const float4*>(s_stat[i % sh.stages]);

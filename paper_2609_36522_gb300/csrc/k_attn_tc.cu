@@ -400,13 +400,13 @@ __global__ void __launch_bounds__(tc_threads<NWG>(), 1)
     Step older, newer;  // (older: L = 2 only)
     int waiting = 0;
     auto second = [&](const Step& e) {
+      if (e.it >= v_seen) {  // without a tile too: every phase is seen, so that a parity means one phase
+        landed(&v_full[e.st], (e.it / sh.stages) & 1u, k_pieces, bad, a.status);
+        v_seen = e.it + 1;
+      }
       if (e.valid) {
         const uint32_t b = L == 1 ? 0 : e.sc & 1u;
         wait_or_bad(&p_full[g][b], (e.sc / L) & 1u, bad, a.status);
-        if (e.it >= v_seen) {
-          landed(&v_full[e.st], (e.it / sh.stages) & 1u, k_pieces, bad, a.status);
-          v_seen = e.it + 1;
-        }
         __syncwarp();
         tc_fence_after_sync();
         if (elect_one()) {
