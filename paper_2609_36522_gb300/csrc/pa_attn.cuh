@@ -122,6 +122,25 @@ __device__ __forceinline__ void mma_over_rows(uint32_t d, uint32_t a, uint64_t b
   for (int k = 0; k < n; ++k, a += 8, b += (uint32_t)sw) tc_mma_f16_ta(d, a, b, idesc, add || k > 0 ? 1u : 0u);
 }
 
+// An A operand in TMEM whose values are held as two 16-bit parts, v = hi + lo to
+// twice the bits: of a block of W columns that were read (32, or 16 for the last
+// ones), the first half holds hi, the second lo. n steps of 16 rows of B.
+__device__ __forceinline__ void mma_parts_over_rows(uint32_t d, uint32_t a, uint64_t b, int sw, int n, uint32_t idesc, bool add) {
+  for (int k = 0; k < n; ++k, b += (uint32_t)sw) {
+    const bool pair = k < (n & ~1);  // a step of a block of 32
+    const uint32_t hi = a + (pair ? (k >> 1) * 32 + (k & 1) * 8 : k * 16), lo = hi + (pair ? 16 : 8);
+    tc_mma_f16_ta(d, hi, b, idesc, add || k > 0 ? 1u : 0u);
+    tc_mma_f16_ta(d, lo, b, idesc, 1u);
+  }
+}
+// Two values as their parts.
+template <typename T>
+__device__ __forceinline__ void two_parts(float x, float y, uint32_t& hi, uint32_t& lo) {
+  hi = Elem<T>::pack2(x, y);
+  const float2 h = Elem<T>::open2(hi);
+  lo = Elem<T>::pack2(x - h.x, y - h.y);
+}
+
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }

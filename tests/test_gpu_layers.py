@@ -132,6 +132,48 @@ def test_norm_rows_through_rings_and_sums_of_their_own(dtype, rows, cols):
     _near(db2, *ref["db"], "db")
 
 
+@pytest.mark.parametrize("dtype,rows,cols", [("fp16", 90001, 64), ("fp16", 5003, 640), ("bf16", 5001, 1024), ("fp32", 30001, 256),
+                                             ("fp32", 5000, 500), ("fp32", 1301, 585), ("fp16", 2003, 257), ("bf16", 1300, 1111),
+                                             ("fp32", 700, 3010), ("bf16", 611, 4099), ("fp16", 320, 8189), ("fp32", 320, 8190)])
+def test_norm_many_rows_of_both_directions(dtype, rows, cols):
+    """Both directions through rings of rows, on 16-byte boundaries and not; strided, over themselves, with a device
+    count, the last row at its tensor's end and beyond it NaN."""
+    from paper_2609_36522_gb300 import layers
+    torch, _ = _torch()
+    x, w, b, dy = _norm_inputs(rows, cols, dtype)
+    _norm_check(x, w, b, dy)
+    _norm_check(x, None, b, dy)
+    ref = _norm_ref(x, w, b, dy, 1e-5)
+    y, mean, rstd = layers.layer_norm(x, w, b, stats=True)
+    dx, dw, db = layers.layer_norm_backward(dy, x, mean, rstd, w)
+    wide, dwide = (torch.full((rows, cols + 8), math.nan, dtype=x.dtype, device="cuda") for _ in range(2))
+    wide[:, :cols] = x
+    dwide[:, :cols] = dy
+    _near(layers.layer_norm(wide[:, :cols], w, b), *ref["y"], "y")
+    got = layers.layer_norm_backward(dwide[:, :cols], wide[:, :cols], mean, rstd, w, dx=dwide[:, :cols])
+    for name, g in zip(("dx", "dw", "db"), got):
+        _near(g, *ref[name], name)
+    assert torch.isnan(dwide[:, cols:]).all()
+    over = x.clone()
+    assert (layers.layer_norm(over, w, b, out=over) == y).all()
+    over = x.clone()
+    again = layers.layer_norm_backward(dy, over, mean, rstd, w, dx=over)
+    assert (over == dx).all() and (again[1] == dw).all() and (again[2] == db).all()
+    only, none, _ = layers.layer_norm_backward(dy, x, mean, rstd, w, weight_grad=False, bias_grad=False)
+    assert none is None
+    _near(only, *ref["dx"], "dx")
+    n = rows - 37
+    count = torch.tensor([n], dtype=torch.int32, device="cuda")
+    out = torch.full_like(x, 7.0)
+    layers.layer_norm(x, w, b, out=out, count=count)
+    assert (out[:n] == y[:n]).all() and (out[n:] == 7.0).all()
+    dx2, dw2, db2 = layers.layer_norm_backward(dy, x, mean, rstd, w, dx=torch.full_like(x, 7.0), count=count)
+    assert (dx2[:n] == dx[:n]).all() and (dx2[n:] == 7.0).all()
+    ref = _norm_ref(x[:n], w, b, dy[:n], 1e-5)
+    _near(dw2, *ref["dw"], "dw")
+    _near(db2, *ref["db"], "db")
+
+
 def test_norm_without_weights_and_single_gradients():
     from paper_2609_36522_gb300 import layers
     x, w, b, dy = _norm_inputs(21, 96, "bf16")
@@ -626,3 +668,20 @@ def test_refusals():
     with pytest.raises(abi.PaError) as e:
         layers.cross_attention(q, k, v, mask=mask, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"), **kw)
     assert e.value.status == abi.PA_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 2, 65, 2, 2, 2, 64), (5, 3, 33, 19, 4, 2, 24), (4, 1, 300, 77, 4, 4, 40),
+                                   (1, 1, 257, 300, 4, 2, 128), (2, 2, 70, 130, 2, 2, 208)])
+def test_attention_gradients_are_as_near_as_their_rounding(shape, dtype):
+    """Probabilities and their gradients enter the second products with 16 bits and more, so nearly all of a gradient's
+    error is that of its last rounding: the norm of the error is at most 1.25 of that of the exact gradient, rounded."""
+    from paper_2609_36522_gb300 import layers
+    q, k, v, do, kw = _attn_inputs(*shape, dtype)
+    ref = _attn_ref(q, k, v, do, scale=shape[6] ** -0.5, **kw)
+    out, lse = layers.cross_attention(q, k, v, stats=True, **kw)
+    got = layers.cross_attention_backward(do, q, k, v, out, lse, **kw)
+    for name, g in zip(("dq", "dk", "dv"), got):
+        want = ref[name][0]
+        rounding = float((want.to(g.dtype).double() - want).norm())
+        assert float((g.double() - want).norm()) <= 1.25 * rounding, name
