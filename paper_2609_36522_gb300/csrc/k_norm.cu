@@ -312,27 +312,28 @@ constexpr int kRingWarps = 8;
 constexpr int kRingStages = 8;            // at most
 constexpr size_t kRingBytes = 108 << 10;  // of a CTA, two to an SM
 
-template <typename T>
+template <typename T, int S>
 struct Ring {
-  const T* x;          // the next stage's rows
-  unsigned char* mem;  // this warp's stages
+  const T* src[S];     // the next stage's rows of each input
+  unsigned char* mem;  // this warp's stages: rows of each input, one behind the other
   uint64_t* full;
   int64_t n, next, hop;  // rows that count; the next stage's first; values from a stage's first row to the next one's
-  int rows, step, cols, stages, bytes, fill, take;
+  int rows, step, cols, stages, bytes, fill, take;  // bytes: of an input's rows
   uint32_t parity;
   bool bad;
 
-  __device__ __forceinline__ Ring(const T* x_, unsigned char* smem, uint64_t (*bars)[kRingStages], int64_t n_, int cols_, int tpr,
+  // full: this warp's barriers
+  __device__ __forceinline__ Ring(const T* const (&in)[S], unsigned char* smem, uint64_t* full_, int64_t n_, int cols_, int tpr,
                                   int stages_)
-      : n(n_), rows(32 / tpr), cols(cols_), stages(stages_), fill(0), take(0), parity(0), bad(false) {
-    const int warp = threadIdx.x >> 5;
+      : full(full_), n(n_), rows(32 / tpr), cols(cols_), stages(stages_), fill(0), take(0), parity(0), bad(false) {
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     bytes = rows * cols * (int)sizeof(T);
-    mem = smem + (size_t)warp * stages * bytes;
-    full = bars[warp];
-    next = ((int64_t)blockIdx.x * kRingWarps + warp) * rows;
-    step = (int)gridDim.x * kRingWarps * rows;
+    mem = smem + (size_t)warp * stages * S * bytes;
+    next = ((int64_t)blockIdx.x * warps + warp) * rows;
+    step = (int)gridDim.x * warps * rows;
     hop = (int64_t)step * cols;
-    x = x_ + next * cols;
+#pragma unroll
+    for (int i = 0; i < S; ++i) src[i] = in[i] + next * cols;
     if ((threadIdx.x & 31) == 0) {
       for (int s = 0; s < stages; ++s) mbar_init(full + s, 1);
       fence_barrier_init();
@@ -340,21 +341,23 @@ struct Ring {
     }
     __syncwarp();
   }
-  __device__ __forceinline__ void request() {  // one lane: the next stage's copy
+  __device__ __forceinline__ void request() {  // one lane: the next stage's copies
     if (next < n) {
       const uint32_t size = next + rows <= n ? (uint32_t)bytes : (uint32_t)((n - next) * cols) * sizeof(T);
-      mbar_arrive_expect_tx(full + fill, size);
-      bulk_g2s(mem + (size_t)fill * bytes, x, size, full + fill);
+      mbar_arrive_expect_tx(full + fill, S * size);
+#pragma unroll
+      for (int i = 0; i < S; ++i) bulk_g2s(mem + (size_t)(fill * S + i) * bytes, src[i], size, full + fill);
     }
     next += step;
-    x += hop;
+#pragma unroll
+    for (int i = 0; i < S; ++i) src[i] += hop;
     if (++fill == stages) fill = 0;
   }
-  // The stage in turn, and that the warp is done with it.
+  // The stage in turn (the first input's rows; `bytes` on, the next one's), and that the warp is done with it.
   __device__ __forceinline__ const T* open(int32_t* status) {
     wait_or_bad(full + take, parity, bad, status);
     __syncwarp();
-    return reinterpret_cast<const T*>(mem + (size_t)take * bytes);
+    return reinterpret_cast<const T*>(mem + (size_t)take * S * bytes);
   }
   __device__ __forceinline__ void close() {
     __syncwarp();
@@ -377,7 +380,8 @@ __global__ void __launch_bounds__(kRingWarps * 32, 2)
   pdl_wait();
   pdl_trigger();
   const int64_t n = counted(rows, count, per);
-  Ring<T> ring(x, smem, bars, n, cols, tpr, stages);
+  const T* const in[1] = {x};
+  Ring<T, 1> ring(in, smem, bars[threadIdx.x >> 5], n, cols, tpr, stages);
   const Rows<false> R(tpr);
   RowSum<false> sum(nullptr, tpr);
   typename P::Raw wv[N], bv[N];
@@ -434,6 +438,288 @@ __global__ void __launch_bounds__(kRingWarps * 32, 2)
         mean[r] = mu;
         rstd[r] = rs;
       }
+    }
+  }
+}
+
+// Backward with dw and db, many rows that lie one behind the other: rings of x and
+// dy, so that the registers are there for the sums: one CTA per SM, with as many
+// warps as have them.
+template <typename T, int N>
+__host__ __device__ constexpr int back_warps() {
+  return N * Elem<T>::kVec <= 16 ? 16 : N * Elem<T>::kVec <= 24 ? 12 : 8;
+}
+constexpr size_t kBackBytes = 208 << 10;
+
+template <typename T, int N>
+__global__ void __launch_bounds__(back_warps<T, N>() * 32, 1)
+    k_norm_ring_bwd(const T* dy, const T* x, const T* __restrict__ w, const float* __restrict__ mean, const float* __restrict__ rstd,
+                    T* dx, int64_t dxs, int64_t rows, int cols, int tpr, const int32_t* count, int64_t per, int stages,
+                    int32_t* status, float* __restrict__ part) {
+  constexpr int V = Elem<T>::kVec, H = N * V / 2;
+  using P = Piece<T, V>;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ __align__(8) uint64_t bars[back_warps<T, N>()][kRingStages];
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = counted(rows, count, per);
+  const T* const in[2] = {x, dy};
+  Ring<T, 2> ring(in, smem, bars[threadIdx.x >> 5], n, cols, tpr, stages);
+  const Rows<false> R(tpr);
+  typename P::Raw wv[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int c = (R.at + i * tpr) * V;
+    wv[i] = w && c < cols ? P::load(w + c) : P::zero();
+  }
+  F2 dw[H], db[H];
+#pragma unroll
+  for (int q = 0; q < H; ++q) dw[q] = db[q] = F2(0.f, 0.f);
+  const float inv = 1.f / (float)cols;
+  const int other = ring.bytes / (int)sizeof(T);
+  int64_t r = R.first;
+  float mu_n = r < n ? mean[r] : 0.f, rs_n = r < n ? rstd[r] : 0.f;
+  for (int64_t lead = R.lead; lead < n; lead += R.step, r += R.step) {
+    const float mu = mu_n, rs = ring.bad ? __int_as_float(0x7fffffff) : rs_n;
+    const int64_t ahead = r + R.step;
+    mu_n = ahead < n ? mean[ahead] : 0.f;
+    rs_n = ahead < n ? rstd[ahead] : 0.f;
+    F2 xh[H], g[H], t1(0.f, 0.f), t2(0.f, 0.f);
+    const F2 nmu(-mu, -mu), rs2(rs, rs);
+    const T* at = ring.open(status) + (int)(r - lead) * cols;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (R.at + i * tpr) * V;
+      const bool there = r < n && c < cols;
+      float xf[V], gf[V], wf[V];
+      P::open(there ? P::load(at + c) : P::zero(), xf);
+      P::open(there ? P::load(at + other + c) : P::zero(), gf);
+      P::open(wv[i], wf);
+#pragma unroll
+      for (int k = 0; k < V; k += 2) {  // beyond the columns and rows dy is 0
+        const int q = (i * V + k) / 2;
+        const F2 d(gf[k], gf[k + 1]);
+        xh[q] = mul2(add2(F2(xf[k], xf[k + 1]), nmu), rs2);
+        dw[q] = fma2(d, xh[q], dw[q]);
+        db[q] = add2(db[q], d);
+        g[q] = w ? mul2(d, F2(wf[k], wf[k + 1])) : d;
+        t1 = add2(t1, g[q]);
+        t2 = fma2(g[q], xh[q], t2);
+      }
+    }
+    ring.close();
+    float s1, s2, a, b;
+    t1.get(a, b);
+    s1 = a + b;
+    t2.get(a, b);
+    s2 = a + b;
+    for (int o = tpr >> 1; o > 0; o >>= 1) {
+      s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+      s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    s1 *= -inv;
+    s2 *= -inv;
+    if (r < n) {
+      const F2 m1(s1, s1), m2(s2, s2);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = (R.at + i * tpr) * V;
+        if (c < cols) {
+          float o[V];
+#pragma unroll
+          for (int k = 0; k < V; k += 2) {
+            const int q = (i * V + k) / 2;
+            mul2(fma2(xh[q], m2, add2(g[q], m1)), rs2).get(o[k], o[k + 1]);
+          }
+          P::store(dx + r * dxs + c, o);
+        }
+      }
+    }
+  }
+  float fw[N * V], fb[N * V];
+#pragma unroll
+  for (int q = 0; q < H; ++q) {
+    dw[q].get(fw[2 * q], fw[2 * q + 1]);
+    db[q].get(fb[2 * q], fb[2 * q + 1]);
+  }
+  __syncthreads();  // the rings' memory is free
+  cta_sums<V, N>(fw, fb, reinterpret_cast<float*>(smem), cols, tpr, R.at, part);
+}
+
+// ---------------------------------------------------------------------------
+// Rows that do not begin on 16 bytes (an odd number of columns): a CTA per row and
+// a ring of rows as the 16-byte units that they lie in, value by value from shared
+// memory. The units at a row's ends are shared with its neighbours, which may be
+// written meanwhile: only the row's own values are looked at. The last row's last unit may
+// pass the tensor's end: its values come by plain loads.
+template <typename T, int S>
+struct Spans {
+  const T* src[S];
+  int64_t stride[S];
+  unsigned char* mem;
+  uint64_t* full;
+  int64_t n, last, next, step;  // rows that count; the tensor's last row; the next one to ask for
+  uint32_t bytes, slot, parity;
+  int stages, fill, take;
+  bool bad;
+
+  static __host__ __device__ uint32_t slot_bytes(int cols) { return (uint32_t)(cols * (int)sizeof(T) + 30) / 16 * 16 + 16; }
+  __device__ __forceinline__ Spans(const T* const (&in)[S], const int64_t (&strides)[S], unsigned char* smem, uint64_t* bars, int64_t n_,
+                                   int64_t rows, int cols, int stages_)
+      : mem(smem), full(bars), n(n_), last(rows - 1), next(blockIdx.x), step(gridDim.x), bytes((uint32_t)cols * sizeof(T)),
+        slot(slot_bytes(cols)), parity(0), stages(stages_), fill(0), take(0), bad(false) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) src[i] = in[i], stride[i] = strides[i];
+    if (threadIdx.x == 0) {
+      for (int s = 0; s < stages; ++s) mbar_init(full + s, 1);
+      fence_barrier_init();
+      for (int s = 0; s < stages; ++s) request();
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ void request() {  // thread 0: the next row
+    if (next < n) {
+      uintptr_t from[S];
+      uint32_t size[S], all = 0;
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
+        const uintptr_t lo = reinterpret_cast<uintptr_t>(src[i] + next * stride[i]), hi = lo + bytes;
+        uintptr_t end = (hi + 15) & ~(uintptr_t)15;
+        from[i] = lo & ~(uintptr_t)15;
+        if (next == last) {
+          end = hi & ~(uintptr_t)15;
+          for (uintptr_t e = end > lo ? end : lo; e < hi; e += sizeof(T))
+            *reinterpret_cast<T*>(mem + (size_t)(fill * S + i) * slot + (e - from[i])) = *reinterpret_cast<const T*>(e);
+        }
+        size[i] = (uint32_t)(end - from[i]);
+        all += size[i];
+      }
+      mbar_arrive_expect_tx(full + fill, all);
+#pragma unroll
+      for (int i = 0; i < S; ++i)
+        if (size[i] > 0) bulk_g2s(mem + (size_t)(fill * S + i) * slot, reinterpret_cast<const void*>(from[i]), size[i], full + fill);
+    }
+    next += step;
+    if (++fill == stages) fill = 0;
+  }
+  __device__ __forceinline__ void wait(int32_t* status) { wait_or_bad(full + take, parity, bad, status); }
+  // Row r of input i, which is in the stage in turn.
+  __device__ __forceinline__ const T* row(int i, int64_t r) const {
+    return reinterpret_cast<const T*>(mem + (size_t)(take * S + i) * slot + (reinterpret_cast<uintptr_t>(src[i] + r * stride[i]) & 15));
+  }
+  // After a barrier behind the last look at the stage.
+  __device__ __forceinline__ void close() {
+    if (threadIdx.x == 0) request();
+    if (++take == stages) {
+      take = 0;
+      parity ^= 1;
+    }
+  }
+};
+
+// N values a thread, as many as leave the fewest threads and idle places: a row
+// then needs no more warps than it has to (barriers), and more rows are worked on at once.
+template <typename T, int N, bool BACK>
+__global__ void __launch_bounds__(kCtaThreads)
+    k_norm_span(const T* x, int64_t xs, const T* dy, int64_t dys, const T* __restrict__ w, const T* __restrict__ b, float eps, T* y,
+                int64_t ys, float* mean, float* rstd, int64_t rows, int cols, const int32_t* count, int64_t per, int stages,
+                int32_t* status, float* __restrict__ part) {
+  constexpr int S = BACK ? 2 : 1;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ __align__(8) uint64_t bars[kRingStages];
+  __shared__ float s_sum[2][64];
+  RowSum<true> sum(s_sum[0], 0), sum2(s_sum[1], 0);
+  pdl_wait();
+  pdl_trigger();
+  const int64_t n = counted(rows, count, per);
+  const T* in[S];
+  int64_t strides[S];
+  in[0] = x;
+  strides[0] = xs;
+  if constexpr (BACK) {
+    in[1] = dy;
+    strides[1] = dys;
+  }
+  Spans<T, S> ring(in, strides, smem, bars, n, rows, cols, stages);
+  const int at = threadIdx.x, t = blockDim.x;
+  const float inv = 1.f / (float)cols;
+  float wv[N], dw[BACK ? N : 1] = {}, db[BACK ? N : 1] = {};
+#pragma unroll
+  for (int i = 0; i < N; ++i) wv[i] = w && at + i * t < cols ? Elem<T>::get(w[at + i * t]) : 1.f;
+  float bv[BACK ? 1 : N] = {};
+  if constexpr (!BACK) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) bv[i] = b && at + i * t < cols ? Elem<T>::get(b[at + i * t]) : 0.f;
+  }
+  float mu_n = 0.f, rs_n = 0.f;
+  if (BACK && blockIdx.x < n) {
+    mu_n = mean[blockIdx.x];
+    rs_n = rstd[blockIdx.x];
+  }
+  for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
+    T* o = y + r * ys;
+    if constexpr (!BACK) {
+      ring.wait(status);
+      const T* p = ring.row(0, r);
+      float v[N], s = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        v[i] = at + i * t < cols ? Elem<T>::get(p[at + i * t]) : 0.f;
+        s += v[i];
+      }
+      const float mu = sum(s) * inv;
+      ring.close();
+      s = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        v[i] -= mu;
+        if (at + i * t < cols) s = fmaf(v[i], v[i], s);
+      }
+      const float rs = ring.bad ? __int_as_float(0x7fffffff) : rsqrtf(sum(s) * inv + eps);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (at + i * t < cols) o[at + i * t] = Elem<T>::put(fmaf(v[i] * rs, wv[i], bv[i]));
+      if (mean && at == 0) {
+        mean[r] = mu;
+        rstd[r] = rs;
+      }
+    } else {
+      const float mu = mu_n, rs = ring.bad ? __int_as_float(0x7fffffff) : rs_n;
+      if (r + gridDim.x < n) {
+        mu_n = mean[r + gridDim.x];
+        rs_n = rstd[r + gridDim.x];
+      }
+      ring.wait(status);
+      const T *p = ring.row(0, r), *q = ring.row(1, r);
+      float xh[N], g[N], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const bool there = at + i * t < cols;
+        xh[i] = there ? (Elem<T>::get(p[at + i * t]) - mu) * rs : 0.f;
+        const float d = there ? Elem<T>::get(q[at + i * t]) : 0.f;
+        dw[i] = fmaf(d, xh[i], dw[i]);
+        db[i] += d;
+        g[i] = d * wv[i];
+        s1 += g[i];
+        s2 = fmaf(g[i], xh[i], s2);
+      }
+      s1 = sum(s1) * inv;
+      s2 = sum2(s2) * inv;
+      ring.close();
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (at + i * t < cols) o[at + i * t] = Elem<T>::put(rs * (g[i] - s1 - xh[i] * s2));
+    }
+  }
+  if constexpr (BACK) {
+    if (part) {
+      float* o = part + (int64_t)blockIdx.x * 2 * cols;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (at + i * t < cols) {
+          o[at + i * t] = dw[i];
+          o[cols + at + i * t] = db[i];
+        }
     }
   }
 }
@@ -678,6 +964,60 @@ cudaError_t ring(const NormArgs& a, const Form& f, cudaStream_t st) {
   return launch_ex(k_norm_ring<T, N>, dim3(152 * 2), dim3(kRingWarps * 32), stages * stage, st, 0, (const T*)a.x, (const T*)a.w,
                    (const T*)a.b, a.eps, (T*)a.y, a.ys, a.mean, a.rstd, a.rows, a.cols, f.tpr, a.count, a.per, stages, a.status);
 }
+template <typename T, int N>
+cudaError_t ring_backward(const NormArgs& a, const Form& f, int* parts, cudaStream_t st) {
+  constexpr int kWarps = back_warps<T, N>();
+  const size_t stage = (size_t)kWarps * (32 / f.tpr) * a.cols * 2 * sizeof(T), fit = kBackBytes / stage;
+  const int stages = fit < kRingStages ? (int)fit : kRingStages;
+  static SmemGranted granted;
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_norm_ring_bwd<T, N>), stages * stage, granted);
+  if (e != cudaSuccess) return e;
+  *parts = 152;
+  return launch_ex(k_norm_ring_bwd<T, N>, dim3(152), dim3(kWarps * 32), stages * stage, st, 0, (const T*)a.dy, (const T*)a.x,
+                   (const T*)a.w, (const float*)a.mean, (const float*)a.rstd, (T*)a.dx, a.dxs, a.rows, a.cols, f.tpr, a.count, a.per,
+                   stages, a.status, a.part);
+}
+// How k_norm_span takes rows: values and threads, CTAs, stages.
+struct SpanForm {
+  int n, threads, grid, stages;
+};
+template <typename T, bool BACK>
+bool spans(const NormArgs& a, const Form& f, SpanForm* s) {
+  if (f.vec || !f.cta || f.n == 0 || !on16(a.x) || (BACK && !on16(a.dy))) return false;
+  if (a.xs < a.cols || (BACK && a.dys < a.cols)) return false;  // a row's last unit lies before the end of the next row
+  const int warps = (a.cols + 32 * 20 - 1) / (32 * 20), each = (a.cols + 32 * warps - 1) / (32 * warps);
+  s->n = each <= 12 ? 12 : each <= 16 ? 16 : 20;
+  s->threads = 32 * warps;
+  int ctas = 16 / warps;  // what 128 registers a thread leave
+  if (ctas < 1) ctas = 1;
+  if (BACK) {  // eight rows to a CTA, so that its sums of dw and db cost little
+    const int64_t most = a.rows / (8 * 152);
+    if (ctas > most) ctas = most < 1 ? 1 : (int)most;
+    if (152 * ctas > norm_parts(a.rows, a.cols)) ctas = norm_parts(a.rows, a.cols) / 152;
+  }
+  const size_t row = (size_t)Spans<T, BACK ? 2 : 1>::slot_bytes(a.cols) * (BACK ? 2 : 1);
+  const auto room = [&] { return (220u << 10) / (unsigned)ctas - 2048u; };  // of a CTA, beside what it holds of its own
+  while (ctas > 1 && 3 * row > room()) --ctas;
+  if (ctas < 1) return false;
+  const size_t fit = room() / row;
+  s->stages = fit < kRingStages ? (int)fit : kRingStages;
+  s->grid = 152 * ctas;
+  return fit >= 2 && a.rows >= 2 * s->grid;
+}
+template <typename T, int N, bool BACK>
+cudaError_t span(const NormArgs& a, const SpanForm& s, cudaStream_t st) {
+  const size_t smem = (size_t)Spans<T, BACK ? 2 : 1>::slot_bytes(a.cols) * (BACK ? 2 : 1) * s.stages;
+  static SmemGranted granted;
+  const cudaError_t e = allow_smem(reinterpret_cast<const void*>(k_norm_span<T, N, BACK>), smem, granted);
+  if (e != cudaSuccess) return e;
+  return launch_ex(k_norm_span<T, N, BACK>, dim3(s.grid), dim3(s.threads), smem, st, 0, (const T*)a.x, a.xs, (const T*)a.dy, a.dys,
+                   (const T*)a.w, (const T*)a.b, a.eps, (T*)(BACK ? a.dx : a.y), BACK ? a.dxs : a.ys, a.mean, a.rstd, a.rows, a.cols,
+                   a.count, a.per, s.stages, a.status, a.part);
+}
+template <typename T, bool BACK>
+cudaError_t span(const NormArgs& a, const SpanForm& s, cudaStream_t st) {
+  return s.n == 12 ? span<T, 12, BACK>(a, s, st) : s.n == 16 ? span<T, 16, BACK>(a, s, st) : span<T, 20, BACK>(a, s, st);
+}
 // Rings fill where every warp has two stages and more; from there on dw and db
 // are worth a pass of their own.
 template <typename T>
@@ -704,7 +1044,33 @@ cudaError_t run(const NormArgs& a, bool back, cudaStream_t st) {
     }
   }
   NormArgs own = a;
-  if (back && a.part && many_rows<T>(a, f)) {  // before dx, which may go over dy or x
+  bool done = false;
+  if (back && a.part && many_rows<T>(a, f) && a.xs == a.cols && a.dys == a.cols) {
+    done = true;
+    switch (f.n) {
+      case 1: e = ring_backward<T, 1>(a, f, &parts, st); break;
+      case 2: e = ring_backward<T, 2>(a, f, &parts, st); break;
+      case 3: e = ring_backward<T, 3>(a, f, &parts, st); break;
+      case 4: e = ring_backward<T, 4>(a, f, &parts, st); break;
+      case 5:
+        if constexpr (V == 4) {
+          e = ring_backward<T, 5>(a, f, &parts, st);
+          break;
+        }
+        [[fallthrough]];
+      default: done = false; break;
+    }
+    if (e != cudaSuccess) return e;
+  }
+  SpanForm sf;
+  if (!back && spans<T, false>(a, f, &sf)) return span<T, false>(a, sf, st);
+  if (back && spans<T, true>(a, f, &sf)) {
+    e = span<T, true>(a, sf, st);
+    if (e != cudaSuccess) return e;
+    done = true;
+    parts = sf.grid;
+  }
+  if (back && !done && a.part && many_rows<T>(a, f)) {  // before dx, which may go over dy or x
     const int gx = (a.cols / V + 31) / 32;
     parts = kMaxParts / gx;
     if (parts < 1) parts = 1;
@@ -715,13 +1081,14 @@ cudaError_t run(const NormArgs& a, bool back, cudaStream_t st) {
   }
   int used = 0;
 #define PA_NORM_CASE(VV, NN, CC) e = back ? backward<T, VV, NN, CC>(own, f, &used, st) : forward<T, VV, NN, CC>(a, f, st)
-  if (f.n == 0) {
+  if (done) {
+  } else if (f.n == 0) {
     const dim3 grid((unsigned)(a.rows < 304 ? a.rows : 304));
     if (!back)
       return launch_ex(k_norm_long<T>, grid, dim3(1024), 0, st, 0, (const T*)a.x, a.xs, (const T*)a.w, (const T*)a.b, a.eps,
                        (T*)a.y, a.ys, a.mean, a.rstd, a.rows, a.cols, a.count, a.per);
     if (a.part) {
-      parts = norm_parts(a.rows) < 64 ? norm_parts(a.rows) : 64;
+      parts = norm_parts(a.rows, a.cols) < 64 ? norm_parts(a.rows, a.cols) : 64;
       e = launch_ex(k_norm_long_sums<T>, dim3((a.cols + kThreads - 1) / kThreads, parts), dim3(kThreads), 0, st, 0,
                     (const T*)a.dy, a.dys, (const T*)a.x, a.xs, (const float*)a.mean, (const float*)a.rstd, a.rows, a.cols,
                     a.count, a.per, a.part);
@@ -748,7 +1115,7 @@ cudaError_t run(const NormArgs& a, bool back, cudaStream_t st) {
     PA_NORM_CASE(1, 8, false);
   }
 #undef PA_NORM_CASE
-  if (own.part && f.n != 0) parts = used;
+  if (own.part && !done && f.n != 0) parts = used;
   if (e != cudaSuccess || !back || !a.part) return e;
   return launch_ex(k_norm_sums<T>, dim3((unsigned)((2 * (int64_t)a.cols + 31) / 32)), dim3(32 * kSumGroups), 0, st, 0,
                    (const float*)a.part, parts, a.cols, (T*)a.dw, (T*)a.db);
@@ -764,7 +1131,10 @@ cudaError_t dispatch(const NormArgs& a, bool back, cudaStream_t st) {
 
 }  // namespace
 
-int norm_parts(int64_t rows) { return rows < kMaxParts ? (int)rows : kMaxParts; }
+int norm_parts(int64_t rows, int cols) {
+  const int most = cols <= 640 ? 16 * 152 : cols <= 1280 ? 8 * 152 : kMaxParts;  // narrow rows: CTAs of a warp or two
+  return rows < most ? (int)rows : most;
+}
 
 cudaError_t launch_norm(const NormArgs& a, cudaStream_t st) { return dispatch(a, false, st); }
 cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t st) { return dispatch(a, true, st); }

@@ -174,7 +174,7 @@ pa_status pa_layer_norm(int dtype, int64_t rows, int cols, const void* x, int64_
 
 size_t pa_layer_norm_backward_workspace_bytes(int64_t rows, int cols) {
   if (rows < 0 || rows > kMaxRows || cols < 1) return 0;
-  return pa::align_up((size_t)(pa::norm_parts(rows) + 1) * 2 * cols * sizeof(float), pa::kAlign);
+  return pa::align_up((size_t)(pa::norm_parts(rows, cols) + 1) * 2 * cols * sizeof(float), pa::kAlign);
 }
 
 pa_status pa_layer_norm_backward(int dtype, int64_t rows, int cols, const void* dy, int64_t dy_stride, const void* x,

@@ -125,7 +125,7 @@ struct NormArgs {
   void *dw, *db;
   float* part;            // partial sums of dw and db
 };
-int norm_parts(int64_t rows);  // rows of partial sums that launch_norm_backward may write, each 2 * cols floats
+int norm_parts(int64_t rows, int cols);  // rows of partial sums that launch_norm_backward may write, each 2 * cols floats
 cudaError_t launch_norm(const NormArgs& a, cudaStream_t st);
 cudaError_t launch_norm_backward(const NormArgs& a, cudaStream_t st);
 
