@@ -138,7 +138,8 @@ template <typename T>
 __device__ __forceinline__ void two_parts(float x, float y, uint32_t& hi, uint32_t& lo) {
   hi = Elem<T>::pack2(x, y);
   const float2 h = Elem<T>::open2(hi);
-  lo = Elem<T>::pack2(x - h.x, y - h.y);
+  add2(F2(x, y), F2(-h.x, -h.y)).get(x, y);
+  lo = Elem<T>::pack2(x, y);
 }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
