@@ -640,8 +640,9 @@ PA_API pa_status pa_gmm_eps_noalloc(const float* means_dev, int K, int64_t D, do
  * kernels). Every tensor is a DEVICE pointer on the current device; its last
  * axis is contiguous and the other strides are given in elements. Arithmetic is
  * fp32, results are rounded once to the tensor's type; of the values in between,
- * the attention's probabilities and their gradients enter the second products
- * in the tensors' 16-bit type. Results do not depend on timing: the same call
+ * the attention's probabilities enter the forward product rounded to the tensors'
+ * 16-bit type, the backward products take them and their gradients as two such
+ * parts. Results do not depend on timing: the same call
  * gives the same bits. Workspaces must be 256-byte aligned and may be reused by
  * the next call on the same stream.
  * ------------------------------------------------------------------------ */
@@ -705,7 +706,8 @@ typedef struct {
   const uint8_t* mask;         /* DEVICE [sources][mask_stride] */
   int64_t mask_stride;
   const int32_t* n_items_dev;  /* DEVICE */
-  void* out;                   /* forward: written; backward: read */
+  void* out;                   /* forward: written; backward: the forward call's (checked; today's kernels take dout . out
+                                  from the probabilities, which the rounding of out does not reach) */
   int64_t out_stride[3];
   float* lse;                  /* [items][tokens][heads]; forward: written, may be NULL; backward: read */
   /* backward only */
@@ -725,8 +727,8 @@ PA_API pa_status pa_attention(const pa_attention_t* a, void* workspace_dev, size
  *   p_i = exp(s_i - lse), ds_i = p_i (dout . v_i - dout . out),
  *   dq = scale sum_i ds_i k_i,  dk_i = scale sum ds_i q,  dv_i = sum p_i dout,
  * the last two over all rows of all items of the source that count and all
- * heads that share the key head. In PA_F16 a value of ds below 2^-24 is lost, as
- * is usual: scale the loss. */
+ * heads that share the key head. In PA_F16 a value of ds below 2^-25 is lost and one
+ * above 65504 overflows, as is usual: scale the loss. */
 PA_API pa_status pa_attention_backward(const pa_attention_t* a, void* workspace_dev, size_t workspace_bytes,
                                        void* stream);
 

@@ -233,6 +233,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
     const int lt = tid - 4 * NWG * 32;
     RowTables<LT> tab{s_rows, 0};
     uint32_t it = 0, qi = 0;
+    Turn kturn(sh.stages), qturn(sh.qbufs);
     int hg = -1, hj = 0;  // the keys that stay
     for (int i = 0, w = blockIdx.x; w < works; ++i, w += gridDim.x) {
       const Work k = work(i, w);
@@ -242,12 +243,12 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
       hj = k.j;
       const T* kp = (const T*)a.k + k.g * a.ks.item + k.j * a.ks.head;
       const T* vp = (const T*)a.v + k.g * a.vs.item + k.j * a.vs.head;
-      const uint32_t qb = qi % sh.qbufs;
+      const uint32_t qb = qturn.at;
       for (int sweep = one ? 1 : 0; sweep < 2; ++sweep) {
         for (int k0 = 0; k0 < k.cnt; k0 += kt) {
           if (!reuse) {
-            const uint32_t st = it % sh.stages;
-            if (it >= (uint32_t)sh.stages) wait_or_bad(&k_empty[st], (it / sh.stages - 1) & 1u, bad, a.status);
+            const uint32_t st = kturn.at;
+            if (it >= (uint32_t)sh.stages) wait_or_bad(&k_empty[st], kturn.parity ^ 1u, bad, a.status);
             const int n = min(kt, k.cnt - k0);
             const uint32_t to = smem_u32(sk + st * 2 * ktile);
             if (sh.k_bulk && (n == kt || !a.len)) {  // past a source's length lies anything: not by whole tiles
@@ -261,9 +262,10 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
               copies_arrive(&k_full[st]);
             }
             ++it;
+            kturn.step();
           }
           if (k0 == 0 && sweep == (one ? 1 : 0)) {
-            if (qi >= (uint32_t)sh.qbufs) wait_or_bad(&q_empty[qb], (qi / sh.qbufs - 1) & 1u, bad, a.status);
+            if (qi >= (uint32_t)sh.qbufs) wait_or_bad(&q_empty[qb], qturn.parity ^ 1u, bad, a.status);
             const T* qp = (const T*)a.q + k.n * a.qs.item + k.j * R * a.qs.head;
             const T* dp = (const T*)a.dout + k.n * a.dos.item + k.j * R * a.dos.head;
 #pragma unroll 1
@@ -287,6 +289,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
         }
       }
       ++qi;
+      qturn.step();
     }
     copies_drain();
   } else {
@@ -296,7 +299,8 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
                    dc0 = tile_desc_cols(smem_u32(sk), box.sw, kt);
     const uint32_t uq = qtile / 16, uk = ktile / 16, tS = taddr + (uint32_t)g * cols;
     const uint32_t idesc2 = tc_idesc_16(128, d16, kBf16, 0, 1);
-    uint32_t it = 0, qi = 0, p_par = 0;
+    uint32_t p_par = 0;
+    Turn kturn(sh.stages), qturn(sh.qbufs);
     int hg = -1, hj = 0;
     bool pv = false, plast = false, pfirst = false, pmul = false, have = false;  // the step before
     uint32_t pst = 0;
@@ -317,26 +321,26 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
       const bool one = k.cnt <= kt, reuse = hg == k.g && hj == k.j, valid = k.group * NWG + g < sh.tiles;
       hg = one ? k.g : -1;
       hj = k.j;
-      const uint32_t qb = qi % sh.qbufs;
+      const uint32_t qb = qturn.at;
       for (int sweep = one ? 1 : 0; sweep < 2; ++sweep) {
         for (int k0 = 0; k0 < k.cnt; k0 += kt) {
           const int n16 = (min(kt, k.cnt - k0) + 15) & ~15;
           const bool begin = k0 == 0 && sweep == (one ? 1 : 0), end = sweep == 1 && k0 + kt >= k.cnt;
           uint32_t st = pst;
           if (!reuse) {
-            st = it % sh.stages;
+            st = kturn.at;
             if (sh.stages == 1 && have) {  // it has to be given back before it can be filled again
               if (pv) second();
               pv = false;
               __syncwarp();
               if (elect_one()) tc_commit(&k_empty[pst]);
             }
-            landed(&k_full[st], (it / sh.stages) & 1u, !sh.k_bulk || a.len, bad, a.status);
+            landed(&k_full[st], kturn.parity, !sh.k_bulk || a.len, bad, a.status);
           }
           if (pv) second();
           pv = valid;
           // without a tile it waits all the same: it must not run ahead of the loaders
-          if (begin) landed(&q_full[qb][g], (qi / sh.qbufs) & 1u, !sh.q_bulk, bad, a.status);
+          if (begin) landed(&q_full[qb][g], qturn.parity, !sh.q_bulk, bad, a.status);
           if (valid) {
             __syncwarp();
             tc_fence_after_sync();
@@ -354,7 +358,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
             if (end) tc_commit(&q_empty[qb]);
           }
           have = true;
-          if (!reuse) ++it;
+          if (!reuse) kturn.step();
           pst = st;
           pn16 = n16;
           pmul = sweep == 1;
@@ -362,7 +366,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
           plast = end;
         }
       }
-      ++qi;
+      qturn.step();
     }
     if (pv) second();
   }
@@ -462,14 +466,15 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
     const float c2 = a.scale * kLog2e;
     const bool live = (warp & 3) * 32 < kn;  // else none of the warp's rows of dv and dk is written: anything may lie in them
     uint32_t par = 0;
-    for (int i = s; i < tiles; i += NS) {
+    Turn turn(sh.stages, s);  // two stages at least
+    for (int i = s; i < tiles; i += NS, turn.step(NS)) {
       wait_or_bad(&s_full[s], par, bad, a.status);
       par ^= 1;
       // lse and delta; after S, which waited for the same phase: the next one cannot have begun
-      wait_or_bad(&q_full[i % sh.stages], (i / sh.stages) & 1u, bad, a.status);
+      wait_or_bad(&q_full[turn.at], turn.parity, bad, a.status);
       __syncwarp();
       tc_fence_after_sync();
-      const float4* st = reinterpret_cast<const float4*>(s_stat[i % sh.stages]);
+      const float4* st = reinterpret_cast<const float4*>(s_stat[turn.at]);
       const F2 c22(c2, c2);
       if (live) columns2<32>(tS, tP, qt, [&](auto& r, auto& d, int c) {
         constexpr int N = sizeof(r) / 4;
@@ -543,9 +548,10 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
       within = (int)(t0 * qt - (int64_t)item * rows_item);
       n = order ? order[i0 + item] : i0 + item;
     }
-    for (int i = 0; i < tiles; ++i) {
-      const uint32_t st = i % sh.stages;
-      if (i >= sh.stages) wait_or_bad(&q_empty[st], (i / sh.stages - 1) & 1u, bad, a.status);
+    Turn turn(sh.stages);
+    for (int i = 0; i < tiles; ++i, turn.step()) {
+      const uint32_t st = turn.at;
+      if (i >= sh.stages) wait_or_bad(&q_empty[st], turn.parity ^ 1u, bad, a.status);
       auto stat_in = [&](const float* f, bool there) {  // row lt's -lse and -delta
 #pragma unroll
         for (int w = 0; w < 2; ++w)
@@ -603,9 +609,10 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
                    dq0 = tile_desc_rows(smem_u32(sq), box.sw);
     const uint32_t uq = qtile / 16, idesc = tc_idesc_16(128, qt, kBf16, 0, 0);
     if (tiles > 0) landed(&k_full, 0, !sh.k_bulk || a.len, bad, a.status);
-    for (int i = 0; i < tiles; ++i) {
-      const uint32_t st = i % sh.stages, s = i % NS, tS = taddr + s * 2 * qt;
-      landed(&q_full[st], (i / sh.stages) & 1u, !sh.q_bulk, bad, a.status);
+    Turn turn(sh.stages);
+    for (int i = 0; i < tiles; ++i, turn.step()) {
+      const uint32_t st = turn.at, s = i % NS, tS = taddr + s * 2 * qt;
+      landed(&q_full[st], turn.parity, !sh.q_bulk, bad, a.status);
       if (i >= NS) wait_or_bad(&s_free[s], (i / NS - 1) & 1u, bad, a.status);
       __syncwarp();
       tc_fence_after_sync();
@@ -619,9 +626,10 @@ __global__ void __launch_bounds__(kDkvThreads, 1)
     // ================= MMAs: dV += P^T dO, dK += dS^T Q =================
     const uint64_t dc0 = tile_desc_cols(smem_u32(sq), box.sw, qt) + (uint32_t)(c0 * 2 / box.sw * (qt * box.sw / 16));
     const uint32_t uq = qtile / 16, idesc = tc_idesc_16(128, dn, kBf16, 0, 1);
-    for (int i = 0; i < tiles; ++i) {
-      const uint32_t st = i % sh.stages, s = i % NS, tS = taddr + s * 2 * qt;
-      landed(&q_full[st], (i / sh.stages) & 1u, !sh.q_bulk, bad, a.status);
+    Turn turn(sh.stages);
+    for (int i = 0; i < tiles; ++i, turn.step()) {
+      const uint32_t st = turn.at, s = i % NS, tS = taddr + s * 2 * qt;
+      landed(&q_full[st], turn.parity, !sh.q_bulk, bad, a.status);
       wait_or_bad(&p_full[s], (i / NS) & 1u, bad, a.status);
       __syncwarp();
       tc_fence_after_sync();

@@ -114,9 +114,14 @@ __device__ __forceinline__ uint64_t tile_desc_cols(uint32_t base, int sw, int ro
 // MMAs of one thread. Over d: n steps of 16 of two tiles of ra and rb rows. Over
 // the rows: n steps of 16 rows, A in TMEM (a step is eight columns).
 __device__ __forceinline__ void mma_over_d(uint32_t d, uint64_t a, int ra, uint64_t b, int rb, int sw, int n, uint32_t idesc) {
-  const int per = sw / 32;
-  for (int k = 0; k < n; a += (uint32_t)(ra * sw / 16), b += (uint32_t)(rb * sw / 16))
-    for (int i = 0; i < per && k < n; ++i, ++k) tc_mma_f16(d, a + 2 * i, b + 2 * i, idesc, k > 0 ? 1u : 0u);
+  const uint32_t per = (uint32_t)sw / 32, ja = (uint32_t)(ra * sw / 16) - 2 * (per - 1), jb = (uint32_t)(rb * sw / 16) - 2 * (per - 1);
+#pragma unroll 4
+  for (uint32_t k = 0; k < (uint32_t)n; ++k) {
+    tc_mma_f16(d, a, b, idesc, k > 0 ? 1u : 0u);
+    const bool last = ((k + 1) & (per - 1)) == 0;
+    a += last ? ja : 2u;
+    b += last ? jb : 2u;
+  }
 }
 __device__ __forceinline__ void mma_over_rows(uint32_t d, uint32_t a, uint64_t b, int sw, int n, uint32_t idesc, bool add) {
   for (int k = 0; k < n; ++k, a += 8, b += (uint32_t)sw) tc_mma_f16_ta(d, a, b, idesc, add || k > 0 ? 1u : 0u);
@@ -126,11 +131,19 @@ __device__ __forceinline__ void mma_over_rows(uint32_t d, uint32_t a, uint64_t b
 // twice the bits: of a block of W columns that were read (32, or 16 for the last
 // ones), the first half holds hi, the second lo. n steps of 16 rows of B.
 __device__ __forceinline__ void mma_parts_over_rows(uint32_t d, uint32_t a, uint64_t b, int sw, int n, uint32_t idesc, bool add) {
-  for (int k = 0; k < n; ++k, b += (uint32_t)sw) {
-    const bool pair = k < (n & ~1);  // a step of a block of 32
-    const uint32_t hi = a + (pair ? (k >> 1) * 32 + (k & 1) * 8 : k * 16), lo = hi + (pair ? 16 : 8);
-    tc_mma_f16_ta(d, hi, b, idesc, add || k > 0 ? 1u : 0u);
-    tc_mma_f16_ta(d, lo, b, idesc, 1u);
+  int k = 0;
+#pragma unroll 2
+  for (; k + 2 <= n; k += 2, a += 32) {
+    tc_mma_f16_ta(d, a, b, idesc, add || k > 0 ? 1u : 0u);
+    tc_mma_f16_ta(d, a + 16, b, idesc, 1u);
+    b += (uint32_t)sw;
+    tc_mma_f16_ta(d, a + 8, b, idesc, 1u);
+    tc_mma_f16_ta(d, a + 24, b, idesc, 1u);
+    b += (uint32_t)sw;
+  }
+  if (k < n) {
+    tc_mma_f16_ta(d, a, b, idesc, add || k > 0 ? 1u : 0u);
+    tc_mma_f16_ta(d, a + 8, b, idesc, 1u);
   }
 }
 // Two values as their parts.
@@ -158,6 +171,20 @@ __device__ __forceinline__ void landed(uint64_t* bar, uint32_t parity, bool piec
   wait_or_bad(bar, parity, bad, status);
   if (pieces) fence_proxy_async_smem();
 }
+
+// A place of a ring of n and the parity of its phase, stepped along: a division by
+// a ring's size takes a lone warp as long as an MMA.
+struct Turn {
+  uint32_t n, at, parity;
+  __device__ __forceinline__ explicit Turn(int n_, int first = 0) : n((uint32_t)n_), at((uint32_t)first), parity(0) {}
+  __device__ __forceinline__ void step(uint32_t by = 1) {  // by <= n
+    at += by;
+    if (at >= n) {
+      at -= n;
+      parity ^= 1u;
+    }
+  }
+};
 
 // Tiled bulk copies: an output or input [item][token][head][d] as a tensor map
 // over (d, head, token, item); a box is `sw` bytes x heads x tokens.
