@@ -84,17 +84,23 @@ __global__ void __launch_bounds__(kListThreads) k_attn_lists(AttnArgs a, int32_t
 // ---------------------------------------------------------------------------
 // CUDA cores: RT rows of one key head per CTA. The lanes of a group of `gs`
 // hold eight values each of a key; a warp works on 32 / gs keys at a time, twice
-// that at once with the next ones on their way, every group with a running maximum
-// and sum of its own; groups and warps are joined at the end. Bound by the reads of
-// the keys and values: what counts is bytes in flight, so registers are kept to two
-// CTAs an SM.
+// that at once, every group with a running maximum and sum of its own; groups and
+// warps are joined at the end. Bound by the reads of the keys and values: what counts
+// is bytes in flight, so a thread's next pieces come by asynchronous copies to places of
+// its own in shared memory, three steps ahead, and nobody waits for anybody.
+// 64 tokens, 4 heads to each of 4 key heads of 64, up to 4096 keys (175 MB): 62 us, 2.8 TB/s (86
+// with the next step in registers); 16 heads of their own (537 MB): 167 us (221). The keys are split to
+// about two CTAs an SM twice over: seven parts of 380 keys instead of three took 12 us more.
 constexpr int kRowWarps = 8;
-constexpr int kRowKeys = 2;  // keys of a group at once
+constexpr int kRowKeys = 2;    // keys of a group at once
+constexpr int kRowStages = 4;  // steps of them
+constexpr int kRowRing = kRowStages * kRowKeys * 2 * kRowWarps * 32 * 16;  // bytes
 
 template <typename T, int RT, int gs>
 __global__ void __launch_bounds__(kRowWarps * 32, 2) k_attn_rows(AttnArgs a, Keys keys, int chunks, int splits,
                                                              float* __restrict__ po, float* __restrict__ pl) {
-  extern __shared__ float smem[];  // [warp][RT][D], then [warp][RT] maxima and sums
+  extern __shared__ __align__(16) unsigned char ring[];  // [stage][key][k, v][thread], 16 bytes each
+  float* smem = reinterpret_cast<float*>(ring + kRowRing);  // [warp][RT][D], then [warp][RT] maxima and sums
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kpw = 32 / gs;
   const int at = lane & (gs - 1), R = a.H / a.J;
@@ -129,43 +135,44 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) k_attn_rows(AttnArgs a, Key
   }
   const T* kp = (const T*)a.k + (int64_t)max(g, 0) * a.ks.item + j * a.ks.head + at * 8;
   const T* vp = (const T*)a.v + (int64_t)max(g, 0) * a.vs.item + j * a.vs.head + at * 8;
-  uint4 ku[kRowKeys], vu[kRowKeys];
   constexpr int stride = kRowWarps * kpw * kRowKeys;
   int next = lo + warp * kpw * kRowKeys + lane / gs;  // this group's next key
   const T *kq = kp + next * a.ks.token, *vq = vp + next * a.vs.token;
   const int64_t kstep = kpw * a.ks.token, vstep = kpw * a.vs.token;
-  auto fetch = [&] {
+  const auto place = [&](uint32_t st, int u, int w) { return ring + (((st * kRowKeys + u) * 2 + w) * (kRowWarps * 32) + threadIdx.x) * 16; };
+  auto fetch = [&](uint32_t st) {
 #pragma unroll
     for (int u = 0; u < kRowKeys; ++u) {
       const int i = next + u * kpw;
-      ku[u] = vu[u] = make_uint4(0, 0, 0, 0);
-      if (i < hi && col) {
-        if (keys.list) {
-          const int64_t key = keys.at(g, i);
-          ku[u] = *reinterpret_cast<const uint4*>(kp + key * a.ks.token);
-          vu[u] = *reinterpret_cast<const uint4*>(vp + key * a.vs.token);
-        } else {
-          ku[u] = *reinterpret_cast<const uint4*>(kq + u * kstep);
-          vu[u] = *reinterpret_cast<const uint4*>(vq + u * vstep);
-        }
+      const bool there = i < hi && col;
+      const T *k = kp, *v = vp;
+      if (there) {
+        const int64_t key = keys.list ? keys.at(g, i) : 0;
+        k = keys.list ? kp + key * a.ks.token : kq + u * kstep;
+        v = keys.list ? vp + key * a.vs.token : vq + u * vstep;
       }
+      copy16(smem_u32(place(st, u, 0)), k, there);
+      copy16(smem_u32(place(st, u, 1)), v, there);
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
     next += stride;
     kq += stride / kpw * kstep;
     vq += stride / kpw * vstep;
   };
   int k0 = lo + warp * kpw * kRowKeys;
-  fetch();
-  for (; k0 < hi; k0 += stride) {
+#pragma unroll
+  for (uint32_t st = 0; st < kRowStages - 1; ++st) fetch(st);
+  for (uint32_t step = 0; k0 < hi; k0 += stride, ++step) {
     uint4 kc[kRowKeys], vc[kRowKeys];
     bool in[kRowKeys];
+    fetch((step + kRowStages - 1) % kRowStages);  // where the step before was
+    asm volatile("cp.async.wait_group %0;" ::"n"(kRowStages - 1) : "memory");
 #pragma unroll
     for (int u = 0; u < kRowKeys; ++u) {
-      kc[u] = ku[u];
-      vc[u] = vu[u];
+      kc[u] = *reinterpret_cast<const uint4*>(place(step % kRowStages, u, 0));
+      vc[u] = *reinterpret_cast<const uint4*>(place(step % kRowStages, u, 1));
       in[u] = k0 + u * kpw + lane / gs < hi;
     }
-    fetch();
     float s[kRowKeys][RT];
 #pragma unroll
     for (int u = 0; u < kRowKeys; ++u) {
@@ -210,6 +217,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) k_attn_rows(AttnArgs a, Key
         for (int i = 0; i < 8; ++i) acc[r][i] = fmaf(s[u][r], vf[i], acc[r][i]);
     }
   }
+  copies_drain();
   // the groups of a warp
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
@@ -310,7 +318,7 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a, int splits, const
 
 // Up to this many query rows of an item and key head the CUDA cores take them, all
 // at once; a tile of the tensor-core kernel has 128, empty or not (four rows against
-// up to 4096 keys of 64: 99 us here, 125 there, and here more rows read the keys again).
+// up to 4096 keys of 64, 64 items: 72 us here, 101 there, and here more rows read the keys again).
 constexpr int kRowsMost = 4;
 
 // How a call is split, and its workspace.
@@ -326,7 +334,7 @@ Plan plan(const AttnArgs& a) {
   p.chunks = (int)((rows + p.rt - 1) / p.rt);
   for (p.gs = 1; p.gs * 8 < a.D;) p.gs <<= 1;
   const int64_t some = (int64_t)a.N * a.J * p.chunks, ctas = some > 0 ? some : 1;
-  const int64_t want = (3 * 608 + ctas - 1) / ctas, most = (a.K + 255) / 256;
+  const int64_t want = (608 + ctas - 1) / ctas, most = (a.K + 255) / 256;
   p.splits = (int)(want < most ? want : most);
   if (p.splits < 1) p.splits = 1;
   p.tc = rows > kRowsMost;
@@ -362,16 +370,18 @@ cudaError_t run(const AttnArgs& a, cudaStream_t st) {
   float* po = reinterpret_cast<float*>(a.ws + p.po);
   float* pl = reinterpret_cast<float*>(a.ws + p.pl);
   const dim3 grid((unsigned)((int64_t)a.N * a.J * p.chunks), p.splits);
-  const size_t smem = (size_t)kRowWarps * p.rt * (a.D + 2) * 4;
+  const size_t smem = kRowRing + (size_t)kRowWarps * p.rt * (a.D + 2) * 4;
   if (p.tc) {
     e = launch_attn_tc(a, keys, po, pl, st);
   } else {
-    const auto go = [&](auto kern) {
-      return launch_ex(kern, grid, dim3(kRowWarps * 32), smem, st, 0, a, keys, p.chunks, p.splits, po, pl);
+    const auto go = [&](auto kern, SmemGranted& granted) {
+      const cudaError_t e = allow_smem(reinterpret_cast<const void*>(kern), smem, granted);
+      return e != cudaSuccess ? e : launch_ex(kern, grid, dim3(kRowWarps * 32), smem, st, 0, a, keys, p.chunks, p.splits, po, pl);
     };
     const auto rows = [&](auto g) {
       constexpr int gs = decltype(g)::value;
-      return p.rt == 1 ? go(k_attn_rows<T, 1, gs>) : go(k_attn_rows<T, 4, gs>);
+      static SmemGranted granted[2];
+      return p.rt == 1 ? go(k_attn_rows<T, 1, gs>, granted[0]) : go(k_attn_rows<T, 4, gs>, granted[1]);
     };
     switch (p.gs) {
       case 1: e = rows(std::integral_constant<int, 1>{}); break;
