@@ -11,6 +11,8 @@
 //               delta = do . out would save the first pass, but out is
 //               rounded to 16 bits: with much of the weight on one key that error is most of
 //               ds (dq off by 6e-3 of its norm against 1.7e-3 for the rounding of dq itself).
+//               It is divided by the row's sum of p, which is 1 but for the rounding of lse:
+//               that of a large lse would be most of ds where one key has nearly all the weight.
 //   k_attn_dkv  a tile of 128 keys and a part of the source's query rows per CTA, the
 //               transposed products S^T = K Q^T and dP^T = V dO^T on 64 query rows at a
 //               time: P^T and dS^T are then A operands where they lie in TMEM, and
@@ -164,7 +166,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
         continue;
       }
       const float l2 = there ? a.lse[((int64_t)k.n * a.Q + t) * a.H + h] * kLog2e : 0.f;
-      float delta = 0.f;
+      float delta = 0.f, all = 0.f;
       const bool one = k.cnt <= kt;
       for (int sweep = one ? 1 : 0; sweep < 2; ++sweep) {
         for (int k0 = 0; k0 < k.cnt; k0 += kt) {
@@ -175,7 +177,7 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
           tc_fence_after_sync();
           const F2 c22(c2, c2), nl2(-l2, -l2);
           if (sweep == 0 || one) {
-            F2 sum(0.f, 0.f);
+            F2 sum(0.f, 0.f), psum(0.f, 0.f);
             columns2<32>(tS, tP, n16, [&](auto& r, auto& d, int c) {
               constexpr int N = sizeof(r) / 4;
               if (c + N > n) {  // exp2 of -infinity: 0
@@ -189,13 +191,17 @@ __global__ void __launch_bounds__(dq_threads<NWG>(), 1)
                 x = ex2(x);
                 y = ex2(y);
                 sum = fma2(F2(x, y), F2(d[q], d[q + 1]), sum);
+                psum = add2(psum, F2(x, y));
               }
             });
             float x, y;
             sum.get(x, y);
             delta += x + y;
+            psum.get(x, y);
+            all += x + y;
           }
           if (sweep == 1) {
+            if (k0 == 0) delta /= all;
             const F2 nd(-delta, -delta);
             columns2<32>(tS, tP, n16, [&](auto& r, auto& d, int c) {
               constexpr int N = sizeof(r) / 4;

@@ -685,3 +685,27 @@ def test_attention_gradients_are_as_near_as_their_rounding(shape, dtype):
         want = ref[name][0]
         rounding = float((want.to(g.dtype).double() - want).norm())
         assert float((g.double() - want).norm()) <= 1.25 * rounding, name
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_attention_gradients_of_a_single_key(dtype):
+    """One key has all of the weight: its score does not matter, so dq and dk are 0 but for the rounding of dout . v,
+    which both differences are made of: within 4 2^-24 of it for dq, and for dk (products the other way round) within the
+    (D + 8) 2^-24 sum |dout||v| that a sum of D terms may be off by in each of the two. Scores are large, so that lse is off by
+    more than that."""
+    from paper_2609_36522_gb300 import layers
+    q, k, v, do, kw = _attn_inputs(3, 2, 200, 1, 4, 2, 64, dtype)
+    q = q * 8
+    scale = 0.5
+    out, lse = layers.cross_attention(q, k, v, scale=scale, stats=True, **kw)
+    dq, dk, dv = layers.cross_attention_backward(do, q, k, v, out, lse, scale=scale, **kw)
+    src = kw["source"].long()
+    kd, vd = (t.double()[src][:, :, :, None].expand(-1, -1, -1, 2, -1).flatten(2, 3) for t in (k, v))  # [items][1][heads][D]
+    dot = (do.double() * vd).sum(-1, keepdim=True).abs()
+    most = (do.double() * vd).abs().sum(-1, keepdim=True)
+    assert float(lse.abs().max()) > 30
+    _near(dq, 0 * q.double(), 1.01 * 4 * E32 * scale * (dot + 72 * E32 * most) * kd.abs() + 2.0 ** -130, "dq")
+    tol = 0 * k.double()
+    each = (2 * 72 + 4) * E32 * scale * most * q.double().abs()
+    tol.index_add_(0, src, each.sum(1, keepdim=True).view(3, 1, 2, 2, 64).sum(3))
+    _near(dk, 0 * k.double(), 1.01 * tol + 2.0 ** -130, "dk")
