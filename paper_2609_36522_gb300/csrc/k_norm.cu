@@ -1139,7 +1139,8 @@ cudaError_t dispatch(const NormArgs& a, bool back, cudaStream_t st) {
 }  // namespace
 
 int norm_parts(int64_t rows, int cols) {
-  const int most = cols <= 640 ? 16 * 152 : cols <= 1280 ? 8 * 152 : kMaxParts;  // narrow rows: CTAs of a warp or two
+  // rows of k_norm_span that take a warp or two: as many CTAs as it may have
+  const int most = cols <= 256 || cols > 1280 ? kMaxParts : cols <= 640 ? 16 * 152 : 8 * 152;
   return rows < most ? (int)rows : most;
 }
 
